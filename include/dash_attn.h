@@ -292,6 +292,108 @@ int dash_attn_fwd_decode_paged(const dash_params* p, const void* Q, const void* 
                                const float* Kbar, const int32_t* kv_len, void* O, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/* ---- Operators around the paged cache: new tokens into the pages, attention of chunks of new tokens, eviction, and the
+ * rotary positions that go with them (also for prefill and training).
+ *
+ * Packed rows: the new tokens of all sequences lie one behind another in tensors [rows, heads, head_dim]; q_start int32
+ * [batch + 1] (device, ascending) says where each sequence's begin, and sequence b has q_len = q_start[b+1] - q_start[b] of
+ * them (0 is allowed).  Rows outside [q_start[0], q_start[batch]) are neither read for a result nor written.
+ * kv_len int32 [batch] (device): cached tokens per sequence INCLUDING the new ones, as for the decode calls: new token i
+ * sits at slot kv_len - q_len + i of its sequence.  A slot below 0 or not below max_pages * page_size does not exist: nothing
+ * is written there and nothing there is attended.
+ * Pages: pools and page_table as in dash_attn_fwd_decode_paged, but page_size may be any multiple of 16.  Table entries
+ * outside [0, num_pages) are never followed: rows for them are dropped, keys and values there read as zeros.  What lies in the
+ * pages behind kv_len may be anything, NaN included. */
+typedef struct dash_paged_params {
+  uint32_t struct_size; /* sizeof(dash_paged_params); checked */
+  int32_t batch;        /* sequences, at most 65535 */
+  int32_t rows;         /* rows of the packed tensors (0 is allowed) */
+  int32_t h_q, h_kv;    /* h_q % h_kv == 0, at most 128 query heads per KV head */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t dtype;        /* dash_dtype of every tensor of queries, keys, values and outputs */
+  int32_t page_size;    /* tokens per page, a multiple of 16 */
+  int32_t max_pages;    /* entries of page_table per sequence; max_pages * page_size at most 2^25 */
+  int32_t num_pages;    /* pages of the pools */
+  int64_t q_stride[2], kn_stride[2], vn_stride[2], o_stride[2]; /* elements (row, head): Q; new K, V; O or rotated Q */
+  int64_t k_stride[3], v_stride[3];                             /* pools: elements (page, token in page, head) */
+} dash_paged_params;
+
+/* Rotary positions with 1 to 4 axes (time, height, width, ...).  Pair i of a head is turned by the angle
+ * positions[axis[i]] * inv_freq[i]:  (x, y) -> (x cos - y sin, x sin + y cos).  The angle is formed as a 64-bit fraction of a
+ * turn, so it is exact to 2^-32 turns at every int32 position.  Elements behind the pairs pass through. */
+typedef struct dash_rope {
+  uint32_t struct_size;   /* sizeof(dash_rope); checked */
+  int32_t pairs;          /* rotated pairs, 1 .. head_dim / 2 */
+  int32_t axes;           /* rows of positions, 1 .. 4 */
+  int32_t interleaved;    /* 0: pair i = elements (i, i + pairs); 1: elements (2i, 2i + 1) */
+  const int32_t* axis;    /* host, pairs entries in [0, axes) */
+  const double* inv_freq; /* host, pairs entries: radians per position, finite */
+} dash_rope;
+
+/* Rotates Q and K of a prefill shape (p->seq_q == p->seq_kv), or with inverse = 1 turns them back: the rotation is orthogonal,
+ * so the backward pass is the inverse applied to the gradients.
+ *   positions  int32 [axes, batch, seq_q], contiguous.
+ *   Q, Qout    by p->q_stride; K, Kout by p->k_stride (either pair may be NULL).  An output may be its own input; it may not
+ *              overlap it otherwise, and output strides of 0 (broadcast) are refused. */
+int dash_attn_rope(const dash_params* p, const dash_rope* rope, const int32_t* positions, const void* Q, const void* K,
+                   void* Qout, void* Kout, int32_t inverse, void* stream);
+
+/* New tokens into the pages: K rows rotated (rope NULL: as they are), V rows as they are, to their slots; Q rows rotated into
+ * Qout (both NULL: keys and values only; Qout may be Q when the strides agree).
+ *   positions  int32 [axes, rows], contiguous (NULL with rope NULL).
+ *   K, V       new rows by p->kn_stride / p->vn_stride; Q by p->q_stride, Qout by p->o_stride.
+ * Two sequences may share pages for reading; where both write the same slot of the same page, either may win. */
+int dash_attn_append_paged(const dash_paged_params* p, const dash_rope* rope, const int32_t* positions,
+                           const int32_t* q_start, const int32_t* kv_len, const int32_t* page_table, const void* Q,
+                           void* Qout, const void* K, const void* V, void* Kpool, void* Vpool, void* stream);
+
+/* Dense causal attention of the new tokens over their sequences' pages (the new tokens' own keys included: append first):
+ *   o_i = sum_{t <= slot(i)} softmax_t(<q_i, k_t> / sqrt(d)) v_t,     lse_i = log sum_{t <= slot(i)} exp(<q_i, k_t> / sqrt(d)).
+ * It serves the layers, and the short contexts, that are not routed, from the cache that dash_attn_fwd_decode_paged reads: one
+ * token per sequence, whole prompts, or both in one call.
+ *   O    by p->o_stride, dtype p->dtype.  A row without a visible key (a slot below 0) gets 0 and lse -inf.
+ *   lse  optional fp32 [rows, h_q], contiguous (natural logarithm); dash_attn_key_mass_paged continues from it.
+ *   workspace  dash_attn_paged_workspace_bytes(p) bytes, 256-byte aligned; it opens with a status word and arrival counters as
+ *              the other workspaces do (dash_attn_reset_status once before the first use; dash_attn_last_status).  Calls that may
+ *              overlap on the GPU need workspaces of their own.
+ * bf16 takes tensor cores (weights rounded to bf16 before they meet V, sums in fp32), fp32 CUDA cores.  The result does not
+ * depend on the other sequences of the call beyond where the sums of a row are split (fp32 rounding). */
+size_t dash_attn_paged_workspace_bytes(const dash_paged_params* p);
+int dash_attn_attend_chunk_paged(const dash_paged_params* p, const void* Q, const void* Kpool, const void* Vpool,
+                                 const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, void* O, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention weight per cached token and KV head, summed over the new rows and the heads of the group:
+ *   mass_out[b, r, t] = decay * mass_in[b, r, t] [t < kv_len - q_len] + sum_{i: slot(i) >= t} sum_{h in group r}
+ *                       exp(<q_ih, k_t> / sqrt(d) - lse_ih),      t < kv_len.
+ *   lse       fp32 [rows, h_q] as dash_attn_attend_chunk_paged writes it for the same Q and pages.
+ *   mass_in, mass_out  fp32 [batch, h_kv, max_pages * page_size], contiguous; mass_in may be NULL (zeros) or mass_out itself.
+ *             Slots of new tokens start from 0 whatever mass_in holds there; slots behind kv_len are left as they are.
+ *   decay     finite; 1 accumulates.
+ * No atomics: every sum has one owner and one order.  Workspace as above (its status word is used). */
+int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const void* Kpool, const int32_t* page_table,
+                             const int32_t* q_start, const int32_t* kv_len, const float* lse, float decay,
+                             const float* mass_in, float* mass_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction: every (sequence, KV head) with more than `keep` cached tokens keeps its first `sinks` slots, its last `recent` and,
+ * up to `keep` in all, the slots in between with the largest mass (equal mass: the lower slot; NaN counts as less than
+ * everything).  The kept tokens move to slots 0, 1, ... in their old order.  Shorter sequences keep everything.
+ *   mass      fp32 [batch, h_kv, max_pages * page_size] (read below kv_len).
+ *   kept      int32 [batch, h_kv, keep], output: old slots, ascending; -1 behind the new length.
+ *   new_len   int32 [batch], output: min(kv_len, keep); may not be kv_len itself.
+ *   Kdst, Vdst, dst_table, dst_max_pages, dst_num_pages   where the kept rows go: pools with the strides of Kpool / Vpool, page
+ *             table [batch, dst_max_pages] with dst_max_pages * page_size >= keep.  Either dst_table == page_table, Kdst == Kpool
+ *             and Vdst == Vpool (in place: the pages must then belong to one sequence each), or no destination page may be a
+ *             page that any sequence of the call is read from.
+ *   mass_out  fp32 [batch, h_kv, dst_max_pages * page_size]: the mass of the kept tokens at their new slots, NULL to skip; may be
+ *             mass itself in place.
+ * Slots at and behind the new length are left as they are.  Chunk summaries of a cache that has moved are stale:
+ * dash_attn_block_summaries_paged makes them anew.  p->rows, p->h_q and the strides of packed tensors are not used. */
+int dash_attn_evict_paged(const dash_paged_params* p, int32_t keep, int32_t sinks, int32_t recent, const float* mass,
+                          const int32_t* kv_len, const int32_t* page_table, const void* Kpool, const void* Vpool,
+                          int32_t* kept, int32_t* new_len, const int32_t* dst_table, int32_t dst_max_pages,
+                          int32_t dst_num_pages, void* Kdst, void* Vdst, float* mass_out, void* stream);
+
 /* Zeroes the status word (enqueued on stream).  Call once after allocating a workspace, and again after an
  * error: the word is sticky (the first error wins), and while it is non-zero the tensor-core kernels launched
  * on that workspace retire without computing, so that one wait that ran out costs one wait limit, not one per

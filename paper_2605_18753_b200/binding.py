@@ -29,6 +29,8 @@ EXPORTS = [
     "dash_attn_bwd_workspace_bytes", "dash_attn_bwd_attend_prefill_tc",
     "dash_attn_block_summaries_paged", "dash_attn_fwd_decode_paged",
     "dash_attn_bwd_select_prefill", "dash_attn_bwd_block_summaries",
+    "dash_attn_rope", "dash_attn_append_paged", "dash_attn_paged_workspace_bytes", "dash_attn_attend_chunk_paged",
+    "dash_attn_key_mass_paged", "dash_attn_evict_paged",
     "dash_attn_fwd_prefill", "dash_attn_fwd_decode", "dash_attn_reset_status", "dash_attn_last_status",
     "dash_attn_launch_count", "dash_attn_strerror", "dash_attn_test_hooks",
 ]
@@ -48,6 +50,20 @@ class DashParams(ctypes.Structure):
         ("local_blocks", c_int32), ("q_to_kv", POINTER(c_int32)),
         ("q_stride", c_int64 * 3), ("k_stride", c_int64 * 3), ("v_stride", c_int64 * 3), ("o_stride", c_int64 * 3),
     ]
+
+
+class DashPagedParams(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", c_uint32), ("batch", c_int32), ("rows", c_int32), ("h_q", c_int32), ("h_kv", c_int32),
+        ("head_dim", c_int32), ("dtype", c_int32), ("page_size", c_int32), ("max_pages", c_int32), ("num_pages", c_int32),
+        ("q_stride", c_int64 * 2), ("kn_stride", c_int64 * 2), ("vn_stride", c_int64 * 2), ("o_stride", c_int64 * 2),
+        ("k_stride", c_int64 * 3), ("v_stride", c_int64 * 3),
+    ]
+
+
+class DashRope(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("pairs", c_int32), ("axes", c_int32), ("interleaved", c_int32),
+                ("axis", POINTER(c_int32)), ("inv_freq", POINTER(ctypes.c_double))]
 
 
 _lib = None
@@ -99,6 +115,19 @@ def lib() -> ctypes.CDLL:
         L.dash_attn_fwd_decode_paged.restype = ctypes.c_int
         L.dash_attn_fwd_decode_paged.argtypes = [P, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
                                                  c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        G, R = POINTER(DashPagedParams), POINTER(DashRope)
+        L.dash_attn_rope.restype = ctypes.c_int
+        L.dash_attn_rope.argtypes = [P, R] + [c_void_p] * 5 + [c_int32, c_void_p]
+        L.dash_attn_append_paged.restype = ctypes.c_int
+        L.dash_attn_append_paged.argtypes = [G, R] + [c_void_p] * 11
+        L.dash_attn_paged_workspace_bytes.restype = c_size_t
+        L.dash_attn_paged_workspace_bytes.argtypes = [G]
+        L.dash_attn_attend_chunk_paged.restype = ctypes.c_int
+        L.dash_attn_attend_chunk_paged.argtypes = [G] + [c_void_p] * 9 + [c_size_t, c_void_p]
+        L.dash_attn_key_mass_paged.restype = ctypes.c_int
+        L.dash_attn_key_mass_paged.argtypes = [G] + [c_void_p] * 6 + [c_float] + [c_void_p] * 3 + [c_size_t, c_void_p]
+        L.dash_attn_evict_paged.restype = ctypes.c_int
+        L.dash_attn_evict_paged.argtypes = [G, c_int32, c_int32, c_int32] + [c_void_p] * 8 + [c_int32, c_int32] + [c_void_p] * 4
         L.dash_attn_reset_status.restype = ctypes.c_int
         L.dash_attn_reset_status.argtypes = [c_void_p, c_void_p]
         L.dash_attn_last_status.restype = ctypes.c_int
@@ -356,6 +385,121 @@ def dash_attn_fwd_decode_paged(p, Q, Kpool, Vpool, page_table, Kbar, kv_len, O, 
                                             Kpool.shape[1], page_table.shape[1], Kpool.shape[0], _ptr(Kbar), _ptr(kv_len),
                                             _ptr(O), _ptr(workspace), workspace.numel(), _stream()),
            "dash_attn_fwd_decode_paged")
+
+
+# ---------------------------------------------------------------- operators around the paged cache
+
+def make_rope(inv_freq, axis=None, interleaved=False) -> DashRope:
+    """Rotary positions: pair i turns by positions[axis[i]] * inv_freq[i] radians (axis None: one axis for all pairs)."""
+    pairs = len(inv_freq)
+    axis = [0] * pairs if axis is None else [int(x) for x in axis]
+    if len(axis) != pairs:
+        raise ValueError("axis and inv_freq must have an entry per pair")
+    r = DashRope()
+    r.struct_size = ctypes.sizeof(DashRope)
+    r.pairs, r.axes, r.interleaved = pairs, max(axis, default=0) + 1, int(bool(interleaved))
+    r.axis = (c_int32 * pairs)(*axis)                                   # (the structure keeps the arrays alive)
+    r.inv_freq = (ctypes.c_double * pairs)(*[float(f) for f in inv_freq])
+    return r
+
+
+def params_for_paged(Kpool, Vpool, page_table, *, h_q, rows=None, Q=None, O=None, K=None, V=None) -> DashPagedParams:
+    """Parameters over pools [num_pages, page_size, h_kv, d] and packed rows Q / O [rows, h_q, d], K / V [rows, h_kv, d].
+    Tensors that are absent count as contiguous; Vpool None stands for the strides of Kpool."""
+    num_pages, page_size, h_kv, d = Kpool.shape
+    packed = [t for t in (Q, O, K, V) if t is not None]
+    if rows is None:
+        rows = packed[0].shape[0] if packed else 0
+    for t, h in ((Q, h_q), (O, h_q), (K, h_kv), (V, h_kv)):
+        if t is not None and (tuple(t.shape) != (rows, h, d) or t.dtype != Kpool.dtype or t.stride(-1) != 1):
+            raise ValueError(f"packed tensors are [rows, heads, head_dim] of the pools' dtype with a contiguous head_dim; got {tuple(t.shape)} {t.dtype}")
+    if Vpool is not None and (Vpool.shape != Kpool.shape or Vpool.dtype != Kpool.dtype):
+        raise ValueError("Kpool and Vpool must agree in shape and dtype")
+    p = DashPagedParams()
+    p.struct_size = ctypes.sizeof(DashPagedParams)
+    p.batch, p.rows, p.h_q, p.h_kv, p.head_dim = page_table.shape[0], rows, h_q, h_kv, d
+    p.dtype = _dtype_code(Kpool.dtype)
+    p.page_size, p.max_pages, p.num_pages = page_size, page_table.shape[1], num_pages
+    for name, t, h in (("q_stride", Q, h_q), ("o_stride", O, h_q), ("kn_stride", K, h_kv), ("vn_stride", V, h_kv)):
+        setattr(p, name, (c_int64 * 2)(*((t.stride(0), t.stride(1)) if t is not None else (h * d, d))))
+    p.k_stride = (c_int64 * 3)(*_strides3(Kpool))
+    p.v_stride = (c_int64 * 3)(*_strides3(Kpool if Vpool is None else Vpool))
+    return p
+
+
+def _check_paged(where, on, ints, floats=()):
+    """The kernels read these tensors as contiguous int32 / fp32 on the current device; another dtype would be misread in silence."""
+    if on.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{where}: the tensors are on device {on.get_device()}, the current device is {torch._C._cuda_getDevice()}")
+    for t in ints:
+        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
+            raise ValueError(f"{where}: positions, q_start, kv_len, page tables and index outputs are contiguous int32 tensors")
+    for t in floats:
+        if t is not None and not (t.dtype is torch.float32 and t.is_contiguous()):
+            raise ValueError(f"{where}: lse and mass are contiguous float32 tensors")
+
+
+def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
+    """Q and K (either may be None) of a prefill shape rotated; inverse=True turns them back, which is the backward pass when it is
+    given the gradients.  positions int32 [axes, batch, seq]; outputs have the strides of their inputs and may be them."""
+    _check_paged("dash_attn_rope", positions, (positions,))
+    if positions.numel() != rope.axes * p.batch * p.seq_q:
+        raise ValueError("positions must be [axes, batch, seq]")
+    _check(lib().dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), _ptr(positions), _ptr(Q), _ptr(K), _ptr(Qout), _ptr(Kout),
+                                int(inverse), _stream()), "dash_attn_rope")
+
+
+def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Qout, K, V, Kpool, Vpool):
+    """Packed new tokens into their pages: K rotated, V as it is, Q rotated into Qout (Q and Qout None: keys and values only;
+    rope and positions None: no rotation)."""
+    _check_paged("dash_attn_append_paged", Kpool, (positions, q_start, kv_len, page_table))
+    if positions is not None and positions.numel() != rope.axes * p.rows:
+        raise ValueError("positions must be [axes, rows]")
+    _check(lib().dash_attn_append_paged(ctypes.byref(p), None if rope is None else ctypes.byref(rope), _ptr(positions), _ptr(q_start),
+                                        _ptr(kv_len), _ptr(page_table), _ptr(Q), _ptr(Qout), _ptr(K), _ptr(V), _ptr(Kpool),
+                                        _ptr(Vpool), _stream()), "dash_attn_append_paged")
+
+
+def dash_attn_paged_workspace_bytes(p: DashPagedParams) -> int:
+    return int(lib().dash_attn_paged_workspace_bytes(ctypes.byref(p)))
+
+
+def alloc_paged_workspace(p: DashPagedParams, device="cuda") -> torch.Tensor:
+    nbytes = dash_attn_paged_workspace_bytes(p)
+    if nbytes == 0:
+        raise DashError(-1, "dash_attn_paged_workspace_bytes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    assert ws.data_ptr() % 256 == 0
+    dash_attn_reset_status(ws)
+    return ws
+
+
+def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len, O, lse, workspace):
+    """Dense causal attention of packed new tokens over their sequences' pages; lse (None to skip) fp32 [rows, h_q]."""
+    _check_paged("dash_attn_attend_chunk_paged", Kpool, (page_table, q_start, kv_len), (lse,))
+    _check(lib().dash_attn_attend_chunk_paged(ctypes.byref(p), _ptr(Q), _ptr(Kpool), _ptr(Vpool), _ptr(page_table), _ptr(q_start),
+                                              _ptr(kv_len), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _stream()),
+           "dash_attn_attend_chunk_paged")
+
+
+def dash_attn_key_mass_paged(p, Q, Kpool, page_table, q_start, kv_len, lse, mass_in, mass_out, workspace, decay=1.0):
+    """Weights that the new rows give every cached token, added to decay * mass_in (None: zeros); fp32 [batch, h_kv, slots]."""
+    _check_paged("dash_attn_key_mass_paged", Kpool, (page_table, q_start, kv_len), (lse, mass_in, mass_out))
+    _check(lib().dash_attn_key_mass_paged(ctypes.byref(p), _ptr(Q), _ptr(Kpool), _ptr(page_table), _ptr(q_start), _ptr(kv_len),
+                                          _ptr(lse), decay, _ptr(mass_in), _ptr(mass_out), _ptr(workspace), workspace.numel(),
+                                          _stream()), "dash_attn_key_mass_paged")
+
+
+def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_len, dst_table, Kdst, Vdst, mass_out=None, *, keep,
+                          sinks=0, recent=0):
+    """Keeps `keep` tokens of every (sequence, KV head) and moves them to the front of the destination pages (page_table, Kpool,
+    Vpool themselves for in place)."""
+    _check_paged("dash_attn_evict_paged", Kpool, (kv_len, page_table, kept, new_len, dst_table), (mass, mass_out))
+    if Kdst.stride() != Kpool.stride() or Vdst.stride() != Vpool.stride() or Kdst.shape[1:] != Kpool.shape[1:] or Kdst.dtype != Kpool.dtype:
+        raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' dtype, page size, heads and strides")
+    _check(lib().dash_attn_evict_paged(ctypes.byref(p), keep, sinks, recent, _ptr(mass), _ptr(kv_len), _ptr(page_table), _ptr(Kpool),
+                                       _ptr(Vpool), _ptr(kept), _ptr(new_len), _ptr(dst_table), dst_table.shape[1], Kdst.shape[0],
+                                       _ptr(Kdst), _ptr(Vdst), _ptr(mass_out), _stream()), "dash_attn_evict_paged")
 
 
 def dash_attn_reset_status(workspace):
