@@ -368,7 +368,10 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
       float m_used = -INFINITY, l = 0.f;
       for (int i = 0; i < steps; ++i) {
         const int j = p.two ? i : 2 * i + s, kv0 = (p.k0 + j) * NT, c = base + j;
-        // Stale rows behind the cache's end must not meet P = 0 as NaN: they are cleared in the tile
+        ok = wait_all(bar(S_FULL + s), (it + i) & 1);      // (the stage's product with V of the step before is done as well)
+        if (!ok) break;
+        // Stale rows behind the cache's end must not meet P = 0 as NaN: they are cleared in the tile.  (Not before the wait above: the
+        // tile before in this place of the ring may not even have arrived, and the phase bit could not tell its load from this one's.)
         if (kv0 + NT > p.s.valid) {
           ok = wait_all(bar(V_FULL + c % VST), (c / VST) & 1);
           if (!ok) break;
@@ -381,8 +384,6 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           }
           ptx::fence_proxy_async_smem();
         }
-        ok = wait_all(bar(S_FULL + s), (it + i) & 1);
-        if (!ok) break;
         if (warp_on) {
           ptx::tc_fence_after();
           uint32_t sr[128];
@@ -416,11 +417,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
             moved = true;
           }
           l *= corr;
-          // O is stable once the stage's previous product has completed
+          // (O is stable: the scores' barrier also stands for every product issued before them)
           if (__any_sync(0xffffffffu, moved) && i > 0) {
-            ok = wait_all(bar(PV_DONE + s), (it + i - 1) & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
 #pragma unroll 1
             for (int q = 0; q < HD / 32; ++q) {
               uint32_t o[32];
@@ -524,6 +522,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         bool last = true;
         if (!whole) {
           if (tid == 0) {
+            __threadfence();                           // the block's results, which meet() has gathered, before the count
             int* counter = arrival_counters(a.sb) + c1st;
             const bool is_last = atomicAdd(counter, 1) == cend - c1st;
             if (is_last) *counter = 0;

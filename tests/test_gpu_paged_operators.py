@@ -179,6 +179,23 @@ def test_long_caches_are_divided_among_blocks(q_lens, kv_lens, dtype):
     c.check_attention()
 
 
+@pytest.mark.parametrize("length", [9 * 128 + 5, 41 * 128 + 42, 70 * 128 + 29])
+def test_tail_of_the_cache_leaves_the_tiles_before_it_alone(length):
+    """Rows behind the end are cleared in the last tile only: the weight of every row sits in the two tiles of 128 slots before it, in
+    rows that the last tile does not have."""
+    b, h_kv = 12, 8
+    c = Cache([1] * b, [length] * b, h_q=16, h_kv=h_kv, d=128, page=64, dtype=BF, seed=length)
+    for k in range(b):
+        for tile in (2, 3):
+            slot = (length // 128 + 1 - tile) * 128 + 60 + 5 * k
+            c.Kc[k][slot] = 0.5 * c.Q[k].view(h_kv, 2, 128)[:, 0].cpu() + 0.5 * c.Q[k].view(h_kv, 2, 128)[:, 1].cpu()
+            c.Kpool[c.table[k, slot // 64].long(), slot % 64] = c.Kc[k][slot].to(DEV)
+    for _ in range(20):
+        c.O.fill_(7.0)
+        c.attend()
+    c.check_attention()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_strided_tensors(dtype):
     """Queries out of a fused projection, outputs and pools with gaps, heads before tokens in the pool."""
