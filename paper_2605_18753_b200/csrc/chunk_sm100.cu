@@ -8,13 +8,13 @@
 // other, each with a warpgroup for its softmax and a quarter-and-a-quarter of tensor memory (S 128 columns, O head_dim columns), so
 // that one stage's MMAs hide the other's exponentials:
 //   a unit of more than TQ tokens: stage 0 and 1 hold its two row tiles, and walk the same K / V tiles;
-//   a unit of at most TQ tokens (decode): both stages hold the same rows and take every other K / V tile; their results are merged.
+//   a unit of at most TQ tokens (decode): both stages hold the same rows and take every other K / V tile; their results are joined.
 //
 // Schedule: the K / V tiles of all units, one behind another, are cut into equal ranges, one per block (a persistent grid of one
-// block per SM).  Sequences of any mix of lengths, one long cache or many short ones, keep every SM busy to the end.  A unit
-// that is cut is finished by the last of its blocks to arrive, which merges the partial results (m, l, O) in the order of the cuts: the
-// result does not depend on which block came last.  Only the two ends of a range can be cut, so partial results take two
-// slots per block, whatever the problem.
+// block per SM).  Sequences of any mix of lengths, one long cache or many short ones, keep every SM busy to the end.  What a block
+// has of a unit that is cut is a partial result (m, l, O); a second kernel joins those of each cut unit in the order of the cuts.
+// Only the two ends of a range can be cut, so partial results take two places per block, whatever the problem.  (Joined by the last
+// block to arrive instead, inside this kernel: 8 to 14 us of fences, counters and dependent loads at the end of every block.)
 //
 // Warp roles (384 threads): warps 0-3 and 4-7 softmax of stage 0 / 1, a row per thread; warp 8 loads Q and K, warp 9 V (TMA, a box
 // per page or per 128 tokens of one), warp 10 issues the MMAs, warp 11 completes the warpgroup for setmaxnreg.  P is written over S in
@@ -32,6 +32,7 @@ namespace {
 
 constexpr int NT = 128;                      // slots per K / V tile
 constexpr int KST = 2, VST = 2;              // ring depths
+constexpr int P_AHEAD = 96;                  // slots of P whose product with V starts before the rest is there
 constexpr int THREADS = 384;
 constexpr int REGS_SOFTMAX = 208, REGS_SERVICE = 88;
 static_assert(256 * REGS_SOFTMAX + 128 * REGS_SERVICE <= THREADS * 168, "what the block was launched with");
@@ -40,14 +41,17 @@ constexpr float RESCALE_LOG2 = 8.f;          // the running maximum moves only w
 constexpr int MAX_SLOTS = 4096;              // unit slots (see the plan) of one launch
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+// Which of the 16 pairs of a tensor-memory load take their exponentials on the FMA pipe (exp2_fma): every fourth.  4096 rows over 16384
+// slots, 32/8 heads, d 128: none 784 us, one in eight 777, in four 761, three in eight 810.
+__host__ __device__ constexpr bool on_fma(int pair) { return pair % 4 == 3; }
+
 enum Bar { Q_FULL = 0, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + KST, V_FULL = K_EMPTY + KST, V_EMPTY = V_FULL + VST, S_FULL = V_EMPTY + VST,
-           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 2, O_FREE = PV_DONE + 2, MERGE = O_FREE + 2, N_BARS };
+           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 4, O_FREE = PV_DONE + 2, MEET = O_FREE + 2, E_DONE, N_BARS = E_DONE + 8 };      // P: [stage][part]; E: [stage][warp]
 
 struct Misc {
   unsigned long long bar[N_BARS];
   uint32_t tmem_base;
   int abort_flag;
-  int last;                                  // this block merges the unit
   int scan[THREADS / 32];
 };
 
@@ -72,6 +76,7 @@ struct ChunkArgs {
   __nv_bfloat16* O;
   float* lse;
   float* partials;
+  struct Cut* cuts;
   StatusBlock* sb;
 };
 
@@ -79,7 +84,6 @@ struct ChunkArgs {
 struct Piece {
   int b, r, t;                     // sequence, KV head, unit of the sequence
   int k0, len, n;                  // first K / V tile and number of them; the unit's
-  long long f0;                    // the unit's first position in the list of all tiles
   Seq s;
   int tokens;                      // of the unit
   bool two;                        // two row tiles; else one, its K / V tiles in turns
@@ -101,33 +105,72 @@ __device__ __forceinline__ int unit_tiles(const PagedDims& pd, const Seq& s, int
   return max(1, (seen + NT - 1) / NT);       // a unit without a key still writes its rows
 }
 
-__device__ __forceinline__ Piece piece_at(const ChunkArgs& a, const Plan& pl, long long f) {
-  Piece p;
-  p.r = (int)(f / pl.total);
-  const int rest = (int)(f - (long long)p.r * pl.total);
-  int lo = 0, hi = a.n_slots;                // last slot with pref <= rest that has tiles
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pl.pref[mid] <= rest) lo = mid; else hi = mid;
+// The pieces of a block's range, in order: a position, from which piece() says the rest (little of it is live inside the loops).
+struct Walk {
+  int left, k0, slot, r;           // tiles left of the range; first tile of the piece, its unit's slot and KV head
+  __device__ __forceinline__ Walk(const ChunkArgs& a, const Plan& pl) {
+    left = (int)(pl.end - pl.begin);
+    k0 = slot = r = 0;
+    if (left <= 0) return;
+    r = (int)(pl.begin / pl.total);
+    const int rest = (int)(pl.begin - (long long)r * pl.total);
+    int lo = 0, hi = a.n_slots;                // last slot with pref <= rest that has tiles
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pl.pref[mid] <= rest) lo = mid; else hi = mid;
+    }
+    slot = lo;
+    k0 = rest - pl.pref[lo];
   }
-  p.b = pl.seq[lo];
-  p.s = load_seq(a.pd, a.q_start, a.kv_len, p.b);
-  const int TT = 2 * a.TQ;
-  p.t = lo + a.slot0 - (p.s.q0 / TT + p.b);
-  p.n = pl.pref[lo + 1] - pl.pref[lo];
-  p.k0 = rest - pl.pref[lo];
-  p.f0 = f - p.k0;
-  p.len = (int)min((long long)(p.n - p.k0), pl.end - f);
-  p.tokens = min(TT, p.s.q_len - p.t * TT);
-  p.two = p.tokens > a.TQ;
-  return p;
-}
+  __device__ __forceinline__ Piece piece(const ChunkArgs& a, const Plan& pl) const {
+    Piece p;
+    p.r = r;
+    p.b = pl.seq[slot];
+    p.s = load_seq(a.pd, a.q_start, a.kv_len, p.b);
+    const int TT = 2 * a.TQ;
+    p.t = slot + a.slot0 - (p.s.q0 / TT + p.b);
+    p.n = pl.pref[slot + 1] - pl.pref[slot];
+    p.k0 = k0;
+    p.len = min(p.n - k0, left);
+    p.tokens = min(TT, p.s.q_len - p.t * TT);
+    p.two = p.tokens > a.TQ;
+    return p;
+  }
+  // Position of the unit's first tile in the list of all tiles.
+  __device__ __forceinline__ long long unit_begin(const Plan& pl) const { return (long long)r * pl.total + pl.pref[slot]; }
+  __device__ __forceinline__ bool done() const { return left <= 0; }
+  __device__ __forceinline__ void next(const ChunkArgs& a, const Plan& pl) {
+    left -= min(pl.pref[slot + 1] - pl.pref[slot] - k0, left);
+    k0 = 0;
+    if (left <= 0) return;
+    do {
+      if (++slot == a.n_slots) {
+        slot = 0;
+        ++r;
+      }
+    } while (pl.pref[slot + 1] == pl.pref[slot]);
+  }
+};
 
-// Partial results of a block: slot 0 a unit begun by an earlier block, 1 one that a later block goes on with, 2 a whole unit in turns.
+// Partial results of a block: place 0 a unit begun by an earlier block, 1 one that later blocks go on with, each for two stages;
+// 2 and 3 in turn the second stage's share of whole units in turns.
+constexpr int PARTS = 6;
 template <int HD> __host__ __device__ constexpr long long partial_floats() { return 128LL * (HD + 2); }
 template <int HD>
-__device__ __forceinline__ float* partial_at(const ChunkArgs& a, int block, int slot, int stage) {
-  return a.partials + (((long long)block * 3 + slot) * 2 + stage) * partial_floats<HD>();
+__device__ __forceinline__ float* partial_at(const ChunkArgs& a, int block, int place, int stage) {
+  return a.partials + ((long long)block * PARTS + (place < 2 ? 2 * place + stage : place + 2)) * partial_floats<HD>();
+}
+
+// What the joining kernel needs to know of the unit that a block cuts at its end.
+struct Cut {
+  int blocks;                      // that hold a part of it (0: the block cuts no unit)
+  int row0, tokens, r, two, pad[3];
+};
+
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __log2f(l)) * LN2 : -INFINITY; }
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -155,7 +198,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
 
   if (tid == 0) {
     misc->abort_flag = (sbase & 1023u) != 0u;
-    for (int i = 0; i < N_BARS; ++i) ptx::mbar_init(bar(i), i >= P_FULL && i < PV_DONE ? 128 : i >= O_FREE && i < MERGE ? 128 : i == MERGE ? 256 : 1);
+    for (int i = 0; i < N_BARS; ++i) ptx::mbar_init(bar(i), i >= P_FULL && i < PV_DONE ? 4 : i >= O_FREE && i < MEET ? 4 : i == MEET ? 8 :
+                                                        i == Q_EMPTY || (i >= K_EMPTY && i < V_FULL) || (i >= V_EMPTY && i < S_FULL) ? 2 : 1);
     ptx::fence_barrier_init();
   }
   if (warp == 10) {
@@ -218,6 +262,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
   pl.begin = blk < G ? blk * pl.all / G : 0;
   pl.end = blk < G ? (blk + 1) * pl.all / G : 0;
 
+  Walk walk(a, pl);
+
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_SERVICE));
     if (warp == 8 || warp == 9) {
@@ -232,8 +278,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
       if (lane == 0) ptx::prefetch_tensormap(tm);
       int cnt = 0, q_cnt = 0;                 // tiles loaded; units
       bool ok = true;
-      for (long long f = pl.begin; f < pl.end && ok;) {
-        const Piece p = piece_at(a, pl, f);
+      for (; ok && !walk.done(); walk.next(a, pl)) {
+        const Piece p = walk.piece(a, pl);
         if (is_k) {
           if (q_cnt > 0) ok = wait_all(bar(Q_EMPTY), (q_cnt - 1) & 1);
           if (!ok) break;
@@ -268,7 +314,6 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
               ptx::tma_load_4d(dst + h * (LY::KV_TILE / (HD / 64)), tm, bar(full + st), h * 64, p.r, tok, page);
           }
         }
-        f += p.len;
       }
       // a wait ran out: let the copies already issued land (bounded) before the block retires
       if (!ok && lane == 0) {
@@ -277,105 +322,137 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         if (is_k && q_cnt > 0)
           for (int k = 0; k < 200000 && !ptx::mbar_try_wait(bar(Q_FULL), (q_cnt - 1) & 1); ++k) {}
       }
-    } else if (warp == 10) {
-      // =========================== MMA issuer ===========================
+    } else {
+      // =========================== MMA issuers: warp 10 stage 0, warp 11 stage 1 ===========================
       constexpr uint32_t IDESC_QK = ptx::idesc_bf16_f32(128, NT, false, false);
       constexpr uint32_t IDESC_PV = ptx::idesc_bf16_f32(128, HD, false, true);
+      const int s = warp - 10;
       const uint64_t qd0 = ptx::smem_desc_sw128(sbase, 16, 1024);
       const uint64_t kd0 = ptx::smem_desc_sw128(sbase + LY::OFF_K, 16, 1024);
       const uint64_t vd0 = ptx::smem_desc_sw128(sbase + LY::OFF_V, NT * 128, 1024);
+      const uint32_t s_tmem = tmem + s * 128, o_tmem = tmem + 256 + s * HD;
       const bool lead = ptx::elect_one();
-      int base = 0, q_cnt = 0;                // K / V tiles of earlier pieces; pieces
-      int it[2] = {0, 0};                     // steps of each stage so far
+      int base = 0, q_cnt = 0, it = 0;        // K / V tiles of earlier pieces; pieces; steps so far
       bool ok = true;
-      for (long long f = pl.begin; f < pl.end && ok;) {
-        const Piece p = piece_at(a, pl, f);
-        const int steps[2] = {p.two ? p.len : (p.len + 1) / 2, p.two ? p.len : p.len / 2};
-        ok = wait_all(bar(Q_FULL), q_cnt & 1);
-        if (!ok) break;
-        auto tile_of = [&](int s, int i) { return base + (p.two ? i : 2 * i + s); };
-        auto qk = [&](int s, int i) -> bool {
-          const int c = tile_of(s, i), st = c % KST;
-          if (!wait_all(bar(K_FULL + st), (c / KST) & 1)) return false;
-          ptx::tc_fence_after();
+      for (; ok && !walk.done(); walk.next(a, pl)) {
+        const Piece p = walk.piece(a, pl);
+        const int steps = p.two ? p.len : s == 0 ? (p.len + 1) / 2 : p.len / 2;
+        const uint64_t qd = qd0 + (uint64_t)((p.two && s ? LY::Q_TILE : 0u) >> 4);
+        auto tile_of = [&](int i) { return base + (p.two ? i : 2 * i + s); };
+        // A tile's place in its ring is free once both stages have said so; in turns one stage says it for both.
+        auto release = [&](int b) {
+          ptx::mma_commit(bar(b));
+          if (!p.two) ptx::mma_commit(bar(b));
+        };
+        auto k_here = [&](int i) {
+          const int c = tile_of(i);
+          return wait_all(bar(K_FULL + c % KST), (c / KST) & 1);
+        };
+        auto qk = [&](int i) {
+          const int st = tile_of(i) % KST;
           if (lead) {
-            const uint64_t qd = qd0 + (uint64_t)((p.two && s ? LY::Q_TILE : 0u) >> 4);
             const uint64_t kd = kd0 + (uint64_t)((st * LY::KV_TILE) >> 4);
 #pragma unroll
             for (int k = 0; k < HD / 16; ++k) {
               const uint64_t off = (uint64_t)(((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4);
-              ptx::mma_bf16_ss(tmem + s * 128, qd + off, kd + off, IDESC_QK, k > 0 ? 1u : 0u);
+              ptx::mma_bf16_ss(s_tmem, qd + off, kd + off, IDESC_QK, k > 0 ? 1u : 0u);
             }
             ptx::mma_commit(bar(S_FULL + s));
-            if (!p.two || s == 1) {
-              ptx::mma_commit(bar(K_EMPTY + st));
-              if (c == base + p.len - 1) ptx::mma_commit(bar(Q_EMPTY));      // the piece's last product with its queries
-            }
+            release(K_EMPTY + st);
+            if (i + 1 == steps) ptx::mma_commit(bar(Q_EMPTY));           // the piece's last product with its queries
           }
           __syncwarp();
-          return true;
         };
-        auto pv = [&](int s, int i) -> bool {
-          const int c = tile_of(s, i), st = c % VST;
-          if (!wait_all(bar(P_FULL + s), (it[s] + i) & 1)) return false;
-          if (!wait_all(bar(V_FULL + st), (c / VST) & 1)) return false;
-          // the first product of a unit overwrites O: its epilogue must have read the last one's
-          if (i == 0 && q_cnt > 0 && !wait_all(bar(O_FREE + s), (q_cnt - 1) & 1)) return false;
-          ptx::tc_fence_after();
-          if (lead) {
-            const uint64_t vd = vd0 + (uint64_t)((st * LY::KV_TILE) >> 4);
-#pragma unroll
-            for (int k = 0; k < NT / 16; ++k)
-              ptx::mma_bf16_ts(tmem + 256 + s * HD, tmem + s * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), IDESC_PV, (i > 0 || k > 0) ? 1u : 0u);
-            ptx::mma_commit(bar(PV_DONE + s));
-            if (!p.two || s == 1) ptx::mma_commit(bar(V_EMPTY + st));
-          }
-          __syncwarp();
-          return true;
-        };
-        ok = qk(0, 0) && (steps[1] == 0 || qk(1, 0));
-        for (int i = 0; i < steps[0] && ok; ++i) {
-          ok = pv(0, i) && (i + 1 >= steps[0] || qk(0, i + 1));
-          if (ok && i < steps[1]) ok = pv(1, i) && (i + 1 >= steps[1] || qk(1, i + 1));
-        }
+        ok = wait_all(bar(Q_FULL), q_cnt & 1) && (steps == 0 || k_here(0));
         if (!ok) break;
+        ptx::tc_fence_after();
+        if (steps > 0) qk(0);
+        else if (lead) ptx::mbar_arrive(bar(Q_EMPTY));
+        for (int i = 0; i < steps; ++i) {
+          // Everything but P is waited for ahead, so that nothing stands between the last half of P and the next scores.
+          const int c = tile_of(i), st = c % VST;
+          ok = wait_all(bar(V_FULL + st), (c / VST) & 1) && (i + 1 == steps || k_here(i + 1));
+          // the first product of a unit overwrites O: its epilogue must have read the last one's
+          if (ok && i == 0 && q_cnt > 0) ok = wait_all(bar(O_FREE + s), (q_cnt - 1) & 1);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (!(ok = ok && wait_all(bar(P_FULL + 2 * s + half), (it + i) & 1))) break;
+            ptx::tc_fence_after();
+            if (lead) {
+              const uint64_t vd = vd0 + (uint64_t)((st * LY::KV_TILE) >> 4);
+#pragma unroll
+              for (int k = 0; k < NT / 16; ++k)
+                if ((k >= P_AHEAD / 16) == (half == 1))
+                  ptx::mma_bf16_ts(o_tmem, s_tmem + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), IDESC_PV, (i > 0 || k > 0) ? 1u : 0u);
+              if (half) {
+                ptx::mma_commit(bar(PV_DONE + s));
+                release(V_EMPTY + st);
+              }
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
+          if (i + 1 < steps) qk(i + 1);
+        }
+        __syncwarp();
         base += p.len;
-        it[0] += steps[0];
-        it[1] += steps[1];
+        it += steps;
         ++q_cnt;
-        f += p.len;
       }
     }
   } else {
-    // =========================== softmax, epilogue, merge ===========================
+    // =========================== softmax, epilogue ===========================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
     const int s = warp >> 2, m = tid & 127;            // stage; row of the tile = TMEM lane
     const int mt = m / g_q, hh = m - mt * g_q;         // token of the row tile, head of the group
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_addr + s * 128, o_addr = lane_addr + 256 + s * HD;
     const float c1 = pd.sm_scale * LOG2E;
-    int base = 0, it = 0, merges = 0;
+    // One arrival per warp: those of 32 lanes are taken one after another.
+    auto arrive = [&](int b) {
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(b));
+    };
+    int base = 0, it = 0, meets = 0, turns = 0;
+    if (tid == 0) a.cuts[blk].blocks = 0;
     bool ok = true;
-    for (long long f = pl.begin; f < pl.end && ok;) {
-      const Piece p = piece_at(a, pl, f);
-      const int steps = p.two ? p.len : s == 0 ? (p.len + 1) / 2 : p.len / 2;
-      const int first = p.two && s ? TQ : 0;           // first token of this stage's rows in the unit
-      const int i_row = p.t * TT + first + mt;
-      const bool row_on = mt < TQ && first + mt < p.tokens;
-      const bool warp_on = __any_sync(0xffffffffu, row_on);
-      // slots that the row sees (rows that are not there never ask for a mask)
-      const int seen = !row_on ? 0x7fffffff : (int)min(max((long long)p.s.kv - p.s.q_len + i_row + 1, 0LL), (long long)p.s.valid);
+    for (; ok && !walk.done(); walk.next(a, pl)) {
       float m_used = -INFINITY, l = 0.f;
-      for (int i = 0; i < steps; ++i) {
-        const int j = p.two ? i : 2 * i + s, kv0 = (p.k0 + j) * NT, c = base + j;
+      int steps, len;
+      bool two, warp_on;
+      {
+      const Piece p = walk.piece(a, pl);
+      two = p.two;
+      len = p.len;
+      steps = two ? len : s == 0 ? (len + 1) / 2 : len / 2;
+      const int first = two && s ? TQ : 0;             // first token of this stage's rows in the unit
+      const bool row_on = mt < TQ && first + mt < p.tokens;
+      warp_on = __any_sync(0xffffffffu, row_on);
+      // Slots that the row sees, from the piece's first tile of this stage on (rows that are not there never ask for a mask), the
+      // fewest of the warp, and the slots that hold anything.
+      const int kv0 = (p.k0 + (two ? 0 : s)) * NT, stride = two ? NT : 2 * NT;
+      int seen = (!row_on ? 0x3fffffff : (int)min(max((long long)p.s.kv - p.s.q_len + p.t * TT + first + mt + 1, 0LL), (long long)p.s.valid)) - kv0;
+      int fewest = __reduce_min_sync(0xffffffffu, seen), held = p.s.valid - kv0, c = base + (two ? 0 : s);
+      // The two warps of a scheduler share its exponential unit.  Left alone they fall into step, both at their exponentials, then both
+      // waiting for products: so they take turns.
+      auto my_turn = [&]() {
+        if (two && (s == 1 || turns > 0)) wait_all(bar(E_DONE + 4 * (1 - s) + (warp & 3)), (s == 1 ? turns : turns - 1) & 1);
+      };
+      auto turn_over = [&]() {
+        if (two) {
+          arrive(E_DONE + 4 * s + (warp & 3));
+          ++turns;
+        }
+      };
+      for (int i = 0; i < steps; ++i, seen -= stride, fewest -= stride, held -= stride, c += two ? 1 : 2) {
         ok = wait_all(bar(S_FULL + s), (it + i) & 1);      // (the stage's product with V of the step before is done as well)
         if (!ok) break;
         // Stale rows behind the cache's end must not meet P = 0 as NaN: they are cleared in the tile.  (Not before the wait above: the
         // tile before in this place of the ring may not even have arrived, and the phase bit could not tell its load from this one's.)
-        if (kv0 + NT > p.s.valid) {
+        if (held < NT) {
           ok = wait_all(bar(V_FULL + c % VST), (c / VST) & 1);
           if (!ok) break;
-          if (kv0 + m >= p.s.valid) {
+          if (m >= held) {
             uint8_t* row = smem + LY::OFF_V + (c % VST) * LY::KV_TILE + m * 128;
 #pragma unroll
             for (int h = 0; h < HD / 64; ++h)
@@ -386,18 +463,17 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         }
         if (warp_on) {
           ptx::tc_fence_after();
-          uint32_t sr[128];
+          uint32_t sr[NT];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < NT / 32; ++q) {
             uint32_t* part = sr + 32 * q;
             DASH_TMEM_LD32(part, s_addr + 32 * q);
           }
           ptx::tmem_wait_ld();
-          const int vis = seen - kv0;
-          if (__any_sync(0xffffffffu, vis < NT)) {
+          if (fewest < NT) {
 #pragma unroll
             for (int k = 0; k < NT; ++k)
-              if (k >= vis) sr[k] = 0xff800000u;       // -inf
+              if (k >= seen) sr[k] = 0xff800000u;       // -inf
           }
           float ch[8];
 #pragma unroll
@@ -429,31 +505,47 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
               DASH_TMEM_ST32(o_addr + q * 32, o);
             }
           }
+          my_turn();
           const float off = m_used == -INFINITY ? 0.f : -m_used;
           const float2 c1v = make_float2(c1, c1), offv = make_float2(off, off);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < NT / 32; ++q) {
             uint32_t pk[16];
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
               const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[32 * q + k]), __uint_as_float(sr[32 * q + k + 1])), c1v, offv);
-              const float2 e = make_float2(exp2f(x.x), exp2f(x.y));
+              const float2 e = on_fma(k >> 1) ? exp2_fma(x) : make_float2(exp2f(x.x), exp2f(x.y));
               sum[(k >> 1) & 1] = __fadd2_rn(sum[(k >> 1) & 1], e);
               const __nv_bfloat162 hv = __floats2bfloat162_rn(e.x, e.y);
               pk[k >> 1] = *reinterpret_cast<const uint32_t*>(&hv);
             }
             ptx::tmem_st_n<16>(s_addr + 16 * q, pk);
+            if (q == P_AHEAD / 32 - 1) {               // the first part goes ahead
+              ptx::tmem_wait_st();
+              ptx::tc_fence_before();
+              arrive(P_FULL + 2 * s);
+            }
           }
+          turn_over();
           const float2 ls = __fadd2_rn(sum[0], sum[1]);
           l += ls.x + ls.y;
           ptx::tmem_wait_st();
           ptx::tc_fence_before();
         }
-        ptx::mbar_arrive(bar(P_FULL + s));
+        if (!warp_on) {
+          my_turn();
+          turn_over();
+          arrive(P_FULL + 2 * s);
+        }
+        arrive(P_FULL + 2 * s + 1);
+      }
       }
       if (!ok) break;
       // ---- the unit's rows, or what this block has of them
+      const Piece p = walk.piece(a, pl);
+      const int first = p.two && s ? TQ : 0, i_row = p.t * TT + first + mt;
+      const bool row_on = mt < TQ && first + mt < p.tokens;
       if (steps > 0) {
         ok = wait_all(bar(PV_DONE + s), (it + steps - 1) & 1);
         if (!ok) break;
@@ -461,116 +553,122 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
       }
       const bool whole = p.len == p.n;
       const long long row = (long long)p.s.q0 + i_row, head = (long long)p.r * g_q + hh;
-      auto lse_of = [&](float mx, float sm) { return sm > 0.f ? (mx + __log2f(sm)) * LN2 : -INFINITY; };
-      auto pack4 = [](float x, float y, float z, float w) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(x, y), hi = __floats2bfloat162_rn(z, w);
-        return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      // Output rows of this thread's group of four lanes (offset in O; -1: not a row).  A store of every lane's own row touches 32 lines
+      // an instruction; four lanes first exchange their 16-byte pieces, then write 64 bytes of each other's rows.
+      long long oofs[4];
+      {
+        const long long mine = row_on ? row * pd.os[0] + head * pd.os[1] : -1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) oofs[k] = __shfl_sync(0xffffffffu, mine, (lane & ~3) + k);
+      }
+      auto store64 = [&](int col, uint32_t (&w)[16]) {         // 32 columns from `col` on, packed; the whole warp
+#pragma unroll
+        for (int step = 1; step < 4; step <<= 1) {
+          const bool up = lane & step;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (k & step) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {                      // piece k of the upper lane against piece k + step of the lower one
+              const uint32_t give = up ? w[k * 4 + q] : w[(k + step) * 4 + q];
+              const uint32_t got = __shfl_xor_sync(0xffffffffu, give, step);
+              if (up) w[k * 4 + q] = got; else w[(k + step) * 4 + q] = got;
+            }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (oofs[k] >= 0)
+            *reinterpret_cast<uint4*>(a.O + oofs[k] + col + (lane & 3) * 8) = make_uint4(w[k * 4], w[k * 4 + 1], w[k * 4 + 2], w[k * 4 + 3]);
+        __syncwarp();
       };
       if (whole && p.two) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        __nv_bfloat16* op = a.O + row * pd.os[0] + head * pd.os[1];
 #pragma unroll 1
         for (int q = 0; q < HD / 32 && warp_on; ++q) {
-          __syncwarp();                                // (rows that are not there skipped the stores of the round before)
-          uint32_t o[32];
+          uint32_t o[32], w[16];
           DASH_TMEM_LD32(o, o_addr + q * 32);
           ptx::tmem_wait_ld();
-          if (row_on) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-              float x[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(o[k + e]) * inv;
-              const uint2 lo = pack4(x[0], x[1], x[2], x[3]), hi = pack4(x[4], x[5], x[6], x[7]);
-              *reinterpret_cast<uint4*>(op + q * 32 + k) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-            }
-          }
+          for (int k = 0; k < 16; ++k) w[k] = pack2(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+          store64(q * 32, w);
         }
         if (row_on && a.lse) a.lse[row * pd.h_q + head] = lse_of(m_used, l);
         ptx::tc_fence_before();
-        ptx::mbar_arrive(bar(O_FREE + s));
+        arrive(O_FREE + s);
       } else {
         // partial result: O unnormalised, four columns of all rows one behind another, then (m, l)
-        const int slot = whole ? 2 : p.k0 > 0 ? 0 : 1;
-        float* part = partial_at<HD>(a, blk, slot, s);
-        if (warp_on) {
+        auto keep_part = [&](float* part) {
+          if (warp_on) {
 #pragma unroll 1
-          for (int q = 0; q < HD / 32 && steps > 0; ++q) {
-            __syncwarp();
-            uint32_t o[32];
-            DASH_TMEM_LD32(o, o_addr + q * 32);
-            ptx::tmem_wait_ld();
-            if (row_on) {
+            for (int q = 0; q < HD / 32 && steps > 0; ++q) {
+              __syncwarp();
+              uint32_t o[32];
+              DASH_TMEM_LD32(o, o_addr + q * 32);
+              ptx::tmem_wait_ld();
+              if (row_on) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 4)
-                __stcg(reinterpret_cast<float4*>(part) + (long long)((q * 32 + k) >> 2) * 128 + m,
-                       make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]), __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])));
-            }
-          }
-          if (row_on) __stcg(reinterpret_cast<float2*>(part + 128 * HD) + m, make_float2(m_used, l));
-        }
-        ptx::tc_fence_before();
-        ptx::mbar_arrive(bar(O_FREE + s));
-        __threadfence();
-        auto meet = [&]() {
-          ptx::mbar_arrive(bar(MERGE));
-          return wait_all(bar(MERGE), merges++ & 1);
-        };
-        if (!(ok = meet())) break;
-        // blocks of the unit, in order: those whose ranges hold its first and its last tile
-        const int c1st = (int)(((p.f0 + 1) * G - 1) / pl.all), cend = (int)(((p.f0 + p.n) * G - 1) / pl.all);
-        bool last = true;
-        if (!whole) {
-          if (tid == 0) {
-            __threadfence();                           // the block's results, which meet() has gathered, before the count
-            int* counter = arrival_counters(a.sb) + c1st;
-            const bool is_last = atomicAdd(counter, 1) == cend - c1st;
-            if (is_last) *counter = 0;
-            __threadfence();
-            misc->last = is_last;
-          }
-          if (!(ok = meet())) break;
-          last = *reinterpret_cast<volatile int*>(&misc->last) != 0;
-          __threadfence();
-        }
-        if (last) {
-          // two row tiles: each warpgroup merges its own; else both share the rows, and every block has two parts of them
-          const int tokens = p.two ? min(TQ, p.tokens - first) : p.tokens, rows = tokens * g_q;
-          const int per = p.two ? 1 : 2, parts = (cend - c1st + 1) * per;
-          auto part_of = [&](int k) {
-            const int cb = c1st + k / per;
-            return partial_at<HD>(a, cb, whole ? 2 : cb == c1st ? 1 : 0, p.two ? s : k % per);
-          };
-          for (int e = p.two ? m : tid; e < rows * (HD / 4); e += p.two ? 128 : 256) {
-            const int mr = e % rows, c4 = e / rows;
-            float mx = -INFINITY, sm = 0.f;
-            for (int k = 0; k < parts; ++k) mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(part_of(k) + 128 * HD) + mr).x);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int k = 0; k < parts; ++k) {
-              const float* src = part_of(k);
-              const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 128 * HD) + mr);
-              if (ml.x > -INFINITY) {
-                const float w = exp2f(ml.x - mx);
-                const float4 o = __ldcg(reinterpret_cast<const float4*>(src) + (long long)c4 * 128 + mr);
-                sm = fmaf(ml.y, w, sm);
-                acc.x = fmaf(o.x, w, acc.x); acc.y = fmaf(o.y, w, acc.y);
-                acc.z = fmaf(o.z, w, acc.z); acc.w = fmaf(o.w, w, acc.w);
+                for (int k = 0; k < 32; k += 4)
+                  __stcg(reinterpret_cast<float4*>(part) + ((q * 32 + k) >> 2) * 128 + m,
+                         make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]), __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])));
               }
             }
-            const float inv = sm > 0.f ? 1.f / sm : 0.f;
-            const int mtok = mr / g_q, mh = mr - mtok * g_q;
-            const long long orow = (long long)p.s.q0 + p.t * TT + first + mtok, ohead = (long long)p.r * g_q + mh;
-            *reinterpret_cast<uint2*>(a.O + orow * pd.os[0] + ohead * pd.os[1] + c4 * 4) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-            if (c4 == 0 && a.lse) a.lse[orow * pd.h_q + ohead] = lse_of(mx, sm);
+            if (row_on) __stcg(reinterpret_cast<float2*>(part + 128 * HD) + m, make_float2(m_used, l));
+          }
+        };
+        if (!whole) {
+          keep_part(partial_at<HD>(a, blk, p.k0 > 0 ? 0 : 1, s));
+          if (tid == 0 && p.k0 == 0) {
+            const long long end = (long long)p.r * pl.total + pl.pref[walk.slot] + p.n;
+            Cut c;
+            c.blocks = (int)((end * G - 1) / pl.all) - blk + 1;      // up to the one whose range holds the unit's last tile
+            c.row0 = p.s.q0 + p.t * TT;
+            c.tokens = p.tokens;
+            c.r = p.r;
+            c.two = p.two;
+            a.cuts[blk] = c;
+          }
+        } else {
+          // a whole unit in turns: the first stage joins what the second has left
+          float* part = partial_at<HD>(a, blk, 2 + (meets & 1), 0);
+          if (s == 1) keep_part(part);
+          __threadfence_block();
+          arrive(MEET);
+          if (!(ok = wait_all(bar(MEET), meets++ & 1))) break;       // (so nobody is more than one such unit ahead: two places do)
+          if (s == 0 && warp_on) {
+            float2 other = make_float2(-INFINITY, 0.f);
+            if (row_on) other = __ldcg(reinterpret_cast<const float2*>(part + 128 * HD) + m);
+            const float top = fmaxf(m_used, other.x);
+            const float w0 = m_used > -INFINITY ? exp2f(m_used - top) : 0.f, w1 = other.x > -INFINITY ? exp2f(other.x - top) : 0.f;
+            const float sm = fmaf(l, w0, other.y * w1), inv = sm > 0.f ? 1.f / sm : 0.f;
+#pragma unroll 1
+            for (int q = 0; q < HD / 32; ++q) {
+              uint32_t o[32], w[16];
+              float4 x[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (w1 > 0.f) x[k] = __ldcg(reinterpret_cast<const float4*>(part) + (q * 8 + k) * 128 + m);
+              }
+              __syncwarp();
+              DASH_TMEM_LD32(o, o_addr + q * 32);
+              ptx::tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float f0 = w0 * inv, f1 = w1 * inv;
+                w[2 * k] = pack2(fmaf(x[k].x, f1, __uint_as_float(o[4 * k]) * f0), fmaf(x[k].y, f1, __uint_as_float(o[4 * k + 1]) * f0));
+                w[2 * k + 1] = pack2(fmaf(x[k].z, f1, __uint_as_float(o[4 * k + 2]) * f0), fmaf(x[k].w, f1, __uint_as_float(o[4 * k + 3]) * f0));
+              }
+              store64(q * 32, w);
+            }
+            if (row_on && a.lse) a.lse[row * pd.h_q + head] = lse_of(top, sm);
           }
         }
-        // slot 2 is written again by this block's next such unit
-        if (whole && !(ok = meet())) break;
+        ptx::tc_fence_before();
+        arrive(O_FREE + s);
       }
       base += p.len;
       it += steps;
-      f += p.len;
     }
     ptx::tc_fence_before();
   }
@@ -581,6 +679,88 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
     ptx::tmem_dealloc(tmem, TMEM_COLS);
   }
   if (tid == 0 && misc->abort_flag) report_error(a.sb, DASH_ERR_TIMEOUT, 301);
+}
+
+// Joins the partial results of a cut unit: block (x, y) the unit that attention block x cuts at its end, 32 columns.  Threads share a
+// row where there are few: P of them take every P-th part each and meet in shared memory.
+constexpr int JOIN_THREADS = 256;
+template <int HD>
+__global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_constant__ ChunkArgs a) {
+  __shared__ float buf[JOIN_THREADS][35];
+  const PagedDims& pd = a.pd;
+  chain_wait();
+  const int first = blockIdx.x, col = blockIdx.y * 32, tid = threadIdx.x;
+  const Cut c = a.cuts[first];
+  if (c.blocks == 0) return;
+  const int per = c.two ? 1 : 2, parts = c.blocks * per;
+  int span = JOIN_THREADS;                   // rows that threads are dealt to
+  if (!c.two)
+    while (span / 2 >= c.tokens * pd.g_q) span >>= 1;
+  const int P = JOIN_THREADS / span, rho = tid & (span - 1);
+  const int stage = c.two ? rho >> 7 : 0, m = c.two ? rho & 127 : rho, token = (c.two ? stage * a.TQ : 0) + m / pd.g_q;
+  const bool on = m < a.TQ * pd.g_q && token < c.tokens;
+  float mx = -INFINITY, sm = 0.f;
+  float4 acc[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (on) {
+#pragma unroll 2
+    for (int k = tid / span; k < parts; k += P) {
+      const float* part = partial_at<HD>(a, first + k / per, k < per ? 1 : 0, c.two ? stage : k % per);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + 128 * HD) + m);
+      float4 x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = __ldcg(reinterpret_cast<const float4*>(part) + (col / 4 + q) * 128 + m);
+      if (ml.x > -INFINITY) {                // (a part without a key has nothing in its place)
+        const float top = fmaxf(mx, ml.x), corr = exp2f(mx - top), w = exp2f(ml.x - top);
+        mx = top;
+        sm = fmaf(ml.y, w, sm * corr);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          acc[q].x = fmaf(x[q].x, w, acc[q].x * corr); acc[q].y = fmaf(x[q].y, w, acc[q].y * corr);
+          acc[q].z = fmaf(x[q].z, w, acc[q].z * corr); acc[q].w = fmaf(x[q].w, w, acc[q].w * corr);
+        }
+      }
+    }
+  }
+  const long long row = (long long)c.row0 + token, head = (long long)c.r * pd.g_q + m % pd.g_q;
+  if (P == 1) {
+    if (!on) return;
+    const float inv = sm > 0.f ? 1.f / sm : 0.f;
+    __nv_bfloat16* op = a.O + row * pd.os[0] + head * pd.os[1] + col;
+#pragma unroll
+    for (int q = 0; q < 8; q += 2)
+      *reinterpret_cast<uint4*>(op + q * 4) = make_uint4(pack2(acc[q].x * inv, acc[q].y * inv), pack2(acc[q].z * inv, acc[q].w * inv),
+                                                         pack2(acc[q + 1].x * inv, acc[q + 1].y * inv), pack2(acc[q + 1].z * inv, acc[q + 1].w * inv));
+    if (col == 0 && a.lse) a.lse[row * pd.h_q + head] = lse_of(mx, sm);
+    return;
+  }
+  buf[tid][32] = mx;
+  buf[tid][33] = sm;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    buf[tid][4 * q] = acc[q].x; buf[tid][4 * q + 1] = acc[q].y; buf[tid][4 * q + 2] = acc[q].z; buf[tid][4 * q + 3] = acc[q].w;
+  }
+  __syncthreads();
+  // a thread per row and pair of columns
+  for (int e = tid; e < span * 16; e += JOIN_THREADS) {
+    const int r2 = e >> 4, q = (e & 15) * 2;
+    if (r2 >= c.tokens * pd.g_q) continue;
+    float top = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
+    for (int k = 0; k < P; ++k) top = fmaxf(top, buf[k * span + r2][32]);
+    for (int k = 0; k < P; ++k) {
+      const float* b = buf[k * span + r2];
+      if (b[32] == -INFINITY) continue;
+      const float w = exp2f(b[32] - top);
+      l = fmaf(b[33], w, l);
+      x = fmaf(b[q], w, x);
+      y = fmaf(b[q + 1], w, y);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const long long orow = (long long)c.row0 + r2 / pd.g_q, ohead = (long long)c.r * pd.g_q + r2 % pd.g_q;
+    *reinterpret_cast<uint32_t*>(a.O + orow * pd.os[0] + ohead * pd.os[1] + col + q) = pack2(x * inv, y * inv);
+    if (col == 0 && q == 0 && a.lse) a.lse[orow * pd.h_q + ohead] = lse_of(top, l);
+  }
 }
 
 // 4-D map of rows [outer][inner][heads][d]: the pool (pages, tokens, heads) or the packed queries (one page of rows).
@@ -603,6 +783,9 @@ cudaError_t launch_hd(ChunkArgs& a, const CUtensorMap& tq, const CUtensorMap& tk
     a.slot0 = (int)s0;
     a.n_slots = (int)(slots - s0 < MAX_SLOTS ? slots - s0 : MAX_SLOTS);
     cudaError_t e = launch_chained(kern, dim3((unsigned)a.n_blocks), dim3(THREADS), Layout<HD>::smem(a.n_slots), st, tq, tk, tv, a);
+    count_launch();
+    if (e != cudaSuccess) return e;
+    e = launch_chained(chunk_join_kernel<HD>, dim3((unsigned)a.n_blocks, HD / 32), dim3(JOIN_THREADS), 0, st, a);
     count_launch();
     if (e != cudaSuccess) return e;
   }
@@ -632,9 +815,10 @@ bool chunk_sm100_supported(const PagedDims& pd) {
   return tensor_map_encoder() != nullptr;
 }
 
-// Two row tiles in three slots of every block; as many blocks as the arrival counters could serve.
+// The cuts, then the blocks' partial results.
 size_t chunk_sm100_partial_bytes(const PagedDims& pd) {
-  return (size_t)256 * 6 * (size_t)(pd.d == 128 ? partial_floats<128>() : partial_floats<64>()) * sizeof(float);
+  const size_t floats = pd.d == 128 ? partial_floats<128>() : partial_floats<64>();
+  return (size_t)current_sm_count() * (sizeof(Cut) + PARTS * floats * sizeof(float));
 }
 
 cudaError_t launch_attend_chunk_sm100(const PagedDims& pd, const void* Q, const void* Kpool, const void* Vpool,
@@ -644,11 +828,12 @@ cudaError_t launch_attend_chunk_sm100(const PagedDims& pd, const void* Q, const 
   a.pd = pd;
   a.TQ = 128 / pd.g_q;
   a.box = paged_box(pd);
-  a.n_blocks = current_sm_count() < 256 ? current_sm_count() : 256;
+  a.n_blocks = current_sm_count();
   a.q_start = q_start; a.kv_len = kv_len; a.page_table = page_table;
   a.O = (__nv_bfloat16*)O;
   a.lse = lse;
-  a.partials = partials;
+  a.cuts = reinterpret_cast<Cut*>(partials);
+  a.partials = partials + (size_t)a.n_blocks * sizeof(Cut) / sizeof(float);
   a.sb = sb;
   CUtensorMap tq, tk, tv;
   if (!paged_q_map(&tq, pd, Q, a.TQ) || !paged_pool_map(&tk, pd, Kpool, pd.ks, a.box) || !paged_pool_map(&tv, pd, Vpool, pd.vs, a.box))
