@@ -136,8 +136,6 @@ struct Walk {
     p.two = p.tokens > a.TQ;
     return p;
   }
-  // Position of the unit's first tile in the list of all tiles.
-  __device__ __forceinline__ long long unit_begin(const Plan& pl) const { return (long long)r * pl.total + pl.pref[slot]; }
   __device__ __forceinline__ bool done() const { return left <= 0; }
   __device__ __forceinline__ void next(const ChunkArgs& a, const Plan& pl) {
     left -= min(pl.pref[slot + 1] - pl.pref[slot] - k0, left);

@@ -93,7 +93,7 @@ cudaError_t launch_attend_chunk_generic(const PagedDims& pd, const void* Q, cons
                                         float* partials, cudaStream_t st);
 cudaError_t launch_key_mass_sm100(const PagedDims& pd, const void* Q, const void* Kpool, const int* page_table, const int* q_start,
                                   const int* kv_len, const float* lse, float decay, const float* mass_in, float* mass_out,
-                                  StatusBlock* sb, cudaStream_t st);
+                                  float* partials, StatusBlock* sb, cudaStream_t st);
 cudaError_t launch_key_mass_generic(const PagedDims& pd, const void* Q, const void* Kpool, const int* page_table,
                                     const int* q_start, const int* kv_len, const float* lse, float decay, const float* mass_in,
                                     float* mass_out, cudaStream_t st);

@@ -183,6 +183,7 @@ int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const vo
   StageRange nv("dash_attn: attention weight per cached token");
   if (pd.dtype == DASH_BF16)
     return cuda_status(launch_key_mass_sm100(pd, Q, Kpool, page_table, q_start, kv_len, lse, decay, mass_in, mass_out,
+                                             reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(STATUS_REGION_BYTES)),
                                              reinterpret_cast<StatusBlock*>(workspace), (cudaStream_t)stream));
   return cuda_status(launch_key_mass_generic(pd, Q, Kpool, page_table, q_start, kv_len, lse, decay, mass_in, mass_out, (cudaStream_t)stream));
 }

@@ -294,6 +294,17 @@ __device__ __forceinline__ void tmem_ld_n(uint32_t* r, uint32_t addr) {
                  : "r"(addr)
                  : "memory");
 }
+// tcgen05.wait::ld for an earlier load of N columns: the registers are in/out operands, so that no use of them moves above it.
+template <int N>
+__device__ __forceinline__ void tmem_wait_ld_regs(uint32_t* r) {
+  if constexpr (N == 32) {
+    DASH_TMEM_WAIT_LD32(r);
+  } else {
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < N; ++k) asm volatile("" : "+r"(r[k]));
+  }
+}
 template <int N>
 __device__ __forceinline__ void tmem_st_n(uint32_t addr, const uint32_t* r) {
   static_assert(N == 2 || N == 4 || N == 8 || N == 16 || N == 32, "supported widths");
