@@ -427,37 +427,78 @@ def params_for_paged(Kpool, Vpool, page_table, *, h_q, rows=None, Q=None, O=None
     return p
 
 
-def _check_paged(where, on, ints, floats=()):
-    """The kernels read these tensors as contiguous int32 / fp32 on the current device; another dtype would be misread in silence."""
-    if on.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{where}: the tensors are on device {on.get_device()}, the current device is {torch._C._cuda_getDevice()}")
-    for t in ints:
-        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
-            raise ValueError(f"{where}: positions, q_start, kv_len, page tables and index outputs are contiguous int32 tensors")
-    for t in floats:
-        if t is not None and not (t.dtype is torch.float32 and t.is_contiguous()):
-            raise ValueError(f"{where}: lse and mass are contiguous float32 tensors")
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _bad(where, t, kind):
+    raise ValueError(f"{where}: expected a contiguous {kind} tensor on the current device, got {t.dtype} on {t.device}, strides {t.stride()}")
+
+
+# The kernels read index tensors as contiguous int32, lse and mass as contiguous fp32, on the current device; anything else would be
+# misread in silence.  (One walk over the arguments gives the addresses as well: 1.5 us of a call's 5.)
+def _i32(where, dev, *ts):
+    out = []
+    for t in ts:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not _I32 or t.get_device() != dev or not t.is_contiguous():
+            _bad(where, t, "int32")
+        out.append(t.data_ptr())
+    return out
+
+
+def _f32(where, dev, *ts):
+    out = []
+    for t in ts:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not _F32 or t.get_device() != dev or not t.is_contiguous():
+            _bad(where, t, "float32")
+        out.append(t.data_ptr())
+    return out
+
+
+def _of(where, dev, dtype, *ts):
+    """Addresses of tensors of queries, keys and values: the parameters' dtype, on the current device."""
+    out = []
+    for t in ts:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not dtype or t.get_device() != dev:
+            raise ValueError(f"{where}: expected {dtype} on the current device, got {t.dtype} on {t.device}")
+        out.append(t.data_ptr())
+    return out
+
+
+_TORCH_DTYPE = {DASH_F32: torch.float32, DASH_BF16: torch.bfloat16}
 
 
 def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
     """Q and K (either may be None) of a prefill shape rotated; inverse=True turns them back, which is the backward pass when it is
     given the gradients.  positions int32 [axes, batch, seq]; outputs have the strides of their inputs and may be them."""
-    _check_paged("dash_attn_rope", positions, (positions,))
+    dev = torch._C._cuda_getDevice()
+    pos, = _i32("dash_attn_rope", dev, positions)
+    q, k, qo, ko = _of("dash_attn_rope", dev, _TORCH_DTYPE[p.dtype], Q, K, Qout, Kout)
     if positions.numel() != rope.axes * p.batch * p.seq_q:
         raise ValueError("positions must be [axes, batch, seq]")
-    _check(lib().dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), _ptr(positions), _ptr(Q), _ptr(K), _ptr(Qout), _ptr(Kout),
-                                int(inverse), _stream()), "dash_attn_rope")
+    if (Q is not None and Qout is not None and Q.stride() != Qout.stride()) or (K is not None and Kout is not None and K.stride() != Kout.stride()):
+        raise ValueError("dash_attn_rope: an output has the strides of its input")
+    _check(lib().dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), pos, q, k, qo, ko, int(inverse), _stream()), "dash_attn_rope")
 
 
 def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Qout, K, V, Kpool, Vpool):
     """Packed new tokens into their pages: K rotated, V as it is, Q rotated into Qout (Q and Qout None: keys and values only;
     rope and positions None: no rotation)."""
-    _check_paged("dash_attn_append_paged", Kpool, (positions, q_start, kv_len, page_table))
+    dev = torch._C._cuda_getDevice()
+    pos, qs, kl, table = _i32("dash_attn_append_paged", dev, positions, q_start, kv_len, page_table)
+    q, qo, k, v, kp, vp = _of("dash_attn_append_paged", dev, _TORCH_DTYPE[p.dtype], Q, Qout, K, V, Kpool, Vpool)
     if positions is not None and positions.numel() != rope.axes * p.rows:
         raise ValueError("positions must be [axes, rows]")
-    _check(lib().dash_attn_append_paged(ctypes.byref(p), None if rope is None else ctypes.byref(rope), _ptr(positions), _ptr(q_start),
-                                        _ptr(kv_len), _ptr(page_table), _ptr(Q), _ptr(Qout), _ptr(K), _ptr(V), _ptr(Kpool),
-                                        _ptr(Vpool), _stream()), "dash_attn_append_paged")
+    _check(lib().dash_attn_append_paged(ctypes.byref(p), None if rope is None else ctypes.byref(rope), pos, qs, kl, table, q, qo, k, v,
+                                        kp, vp, _stream()), "dash_attn_append_paged")
 
 
 def dash_attn_paged_workspace_bytes(p: DashPagedParams) -> int:
@@ -476,30 +517,36 @@ def alloc_paged_workspace(p: DashPagedParams, device="cuda") -> torch.Tensor:
 
 def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len, O, lse, workspace):
     """Dense causal attention of packed new tokens over their sequences' pages; lse (None to skip) fp32 [rows, h_q]."""
-    _check_paged("dash_attn_attend_chunk_paged", Kpool, (page_table, q_start, kv_len), (lse,))
-    _check(lib().dash_attn_attend_chunk_paged(ctypes.byref(p), _ptr(Q), _ptr(Kpool), _ptr(Vpool), _ptr(page_table), _ptr(q_start),
-                                              _ptr(kv_len), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _stream()),
-           "dash_attn_attend_chunk_paged")
+    dev = torch._C._cuda_getDevice()
+    table, qs, kl = _i32("dash_attn_attend_chunk_paged", dev, page_table, q_start, kv_len)
+    ls, = _f32("dash_attn_attend_chunk_paged", dev, lse)
+    q, kp, vp, o = _of("dash_attn_attend_chunk_paged", dev, _TORCH_DTYPE[p.dtype], Q, Kpool, Vpool, O)
+    _check(lib().dash_attn_attend_chunk_paged(ctypes.byref(p), q, kp, vp, table, qs, kl, o, ls, workspace.data_ptr(), workspace.numel(),
+                                              _stream()), "dash_attn_attend_chunk_paged")
 
 
 def dash_attn_key_mass_paged(p, Q, Kpool, page_table, q_start, kv_len, lse, mass_in, mass_out, workspace, decay=1.0):
     """Weights that the new rows give every cached token, added to decay * mass_in (None: zeros); fp32 [batch, h_kv, slots]."""
-    _check_paged("dash_attn_key_mass_paged", Kpool, (page_table, q_start, kv_len), (lse, mass_in, mass_out))
-    _check(lib().dash_attn_key_mass_paged(ctypes.byref(p), _ptr(Q), _ptr(Kpool), _ptr(page_table), _ptr(q_start), _ptr(kv_len),
-                                          _ptr(lse), decay, _ptr(mass_in), _ptr(mass_out), _ptr(workspace), workspace.numel(),
-                                          _stream()), "dash_attn_key_mass_paged")
+    dev = torch._C._cuda_getDevice()
+    table, qs, kl = _i32("dash_attn_key_mass_paged", dev, page_table, q_start, kv_len)
+    ls, mi, mo = _f32("dash_attn_key_mass_paged", dev, lse, mass_in, mass_out)
+    q, kp = _of("dash_attn_key_mass_paged", dev, _TORCH_DTYPE[p.dtype], Q, Kpool)
+    _check(lib().dash_attn_key_mass_paged(ctypes.byref(p), q, kp, table, qs, kl, ls, decay, mi, mo, workspace.data_ptr(),
+                                          workspace.numel(), _stream()), "dash_attn_key_mass_paged")
 
 
 def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_len, dst_table, Kdst, Vdst, mass_out=None, *, keep,
                           sinks=0, recent=0):
     """Keeps `keep` tokens of every (sequence, KV head) and moves them to the front of the destination pages (page_table, Kpool,
     Vpool themselves for in place)."""
-    _check_paged("dash_attn_evict_paged", Kpool, (kv_len, page_table, kept, new_len, dst_table), (mass, mass_out))
-    if Kdst.stride() != Kpool.stride() or Vdst.stride() != Vpool.stride() or Kdst.shape[1:] != Kpool.shape[1:] or Kdst.dtype != Kpool.dtype:
-        raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' dtype, page size, heads and strides")
-    _check(lib().dash_attn_evict_paged(ctypes.byref(p), keep, sinks, recent, _ptr(mass), _ptr(kv_len), _ptr(page_table), _ptr(Kpool),
-                                       _ptr(Vpool), _ptr(kept), _ptr(new_len), _ptr(dst_table), dst_table.shape[1], Kdst.shape[0],
-                                       _ptr(Kdst), _ptr(Vdst), _ptr(mass_out), _stream()), "dash_attn_evict_paged")
+    dev = torch._C._cuda_getDevice()
+    kl, table, kept_at, len_at, dst = _i32("dash_attn_evict_paged", dev, kv_len, page_table, kept, new_len, dst_table)
+    m, mo = _f32("dash_attn_evict_paged", dev, mass, mass_out)
+    kp, vp, kd, vd = _of("dash_attn_evict_paged", dev, _TORCH_DTYPE[p.dtype], Kpool, Vpool, Kdst, Vdst)
+    if Kdst.stride() != Kpool.stride() or Vdst.stride() != Vpool.stride() or Kdst.shape[1:] != Kpool.shape[1:]:
+        raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' page size, heads and strides")
+    _check(lib().dash_attn_evict_paged(ctypes.byref(p), keep, sinks, recent, m, kl, table, kp, vp, kept_at, len_at, dst, dst_table.shape[1],
+                                       Kdst.shape[0], kd, vd, mo, _stream()), "dash_attn_evict_paged")
 
 
 def dash_attn_reset_status(workspace):

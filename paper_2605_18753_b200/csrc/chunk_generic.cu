@@ -4,7 +4,7 @@
 // threads as 16 x 16, a thread's scores are ROWS / 16 rows by 4 slots, its outputs ROWS / 16 rows by head_dim / 16 columns, both fed
 // by 16-byte reads of shared memory (64 FMAs per 8 reads at ROWS = 64).  ROWS = 16 serves calls with few new tokens per sequence,
 // where 64 would be mostly empty.  Few units split their slots over blocks (partial m, l, O, joined by a second kernel).
-// Bound by FFMA issue and the shared-memory reads that feed it.
+// Tiles come by asynchronous copies behind the arithmetic.  Bound by FFMA issue and the shared-memory reads that feed it.
 #include "paged.cuh"
 
 namespace dash {
@@ -32,21 +32,41 @@ __device__ __forceinline__ long long slot_base(const GenArgs& a, int b, int rows
   return (long long)q0 * a.pd.g_q / rows_per + b;
 }
 
+// Asynchronous copies into shared memory, 16 bytes each (src null: zeros; `any` is then a valid address that is not read), in groups.
+__device__ __forceinline__ void copy16(float* dst, const float* src, const float* any) {
+  const int bytes = src ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src ? src : any), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Where the 64 slots of a tile lie (page, token; page -1: nowhere), worked out by 64 threads a tile ahead and kept in the padding of the K
+// rows, two tiles in turn.  (Worked out by every thread for its own copies, a trip to the page table stood before each of them.)
+template <int D>
+__device__ __forceinline__ int2* where(float* ks, int t, int parity) { return reinterpret_cast<int2*>(ks + t * (D + 4) + D) + parity; }
+struct Where {
+  int lp, tok, ph;
+  __device__ __forceinline__ Where(const PagedDims& pd, const int* table, int slot, int valid) : lp(-1), tok(0), ph(-1) {
+    if (slot >= valid) return;
+    lp = slot / pd.page_size;
+    tok = slot - lp * pd.page_size;
+    ph = __ldg(table + lp);
+  }
+  __device__ __forceinline__ int2 get(const PagedDims& pd) const { return make_int2(ph >= 0 && ph < pd.num_pages ? ph : -1, tok); }
+};
+
 // 64 rows of K or V of one (sequence, KV head) into shared memory, row stride LD; slots without a key are zeros.
 template <int D, int LD>
-__device__ __forceinline__ void load_tile(const PagedDims& pd, const float* pool, const long long* st, const int* table, int r, int kv0, int valid,
-                                          float* dst) {
+__device__ __forceinline__ void load_tile(const PagedDims& pd, const float* pool, const long long* st, int r, float* ks, int parity, float* dst) {
   constexpr int V4 = D / 4;
+  pool += r * st[2];
+#pragma unroll 4
   for (int k = threadIdx.x; k < KT * V4; k += THREADS) {
-    const int t = k / V4, c = k - t * V4, slot = kv0 + t;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (slot < valid) {
-      const int lp = slot / pd.page_size, ph = __ldg(table + lp);
-      if (ph >= 0 && ph < pd.num_pages)
-        x = __ldg(reinterpret_cast<const float4*>(pool + (long long)ph * st[0] + (long long)(slot - lp * pd.page_size) * st[1] + r * st[2]) + c);
-    }
-    *reinterpret_cast<float4*>(dst + t * LD + c * 4) = x;
+    const int t = k / V4, c = k - t * V4;
+    const int2 at = *where<D>(ks, t, parity);
+    copy16(dst + t * LD + c * 4, at.x >= 0 ? pool + at.x * st[0] + at.y * st[1] + c * 4 : nullptr, pool);
   }
+  copies_issued();
 }
 
 // Query rows first .. first + ROWS - 1 of the sequence's (token, head) rows; rows behind the last are zeros.
@@ -57,13 +77,14 @@ __device__ __forceinline__ void load_rows(const PagedDims& pd, const float* Q, c
   for (int k = threadIdx.x; k < ROWS * V4; k += THREADS) {
     const int m = k / V4, c = k - m * V4;
     const long long rho = first + m;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* src = nullptr;
     if (rho < n) {
-      const int tok = (int)(rho / pd.g_q), hh = (int)(rho - (long long)tok * pd.g_q);
-      x = __ldg(reinterpret_cast<const float4*>(Q + (long long)(s.q0 + tok) * pd.qs[0] + (long long)(r * pd.g_q + hh) * pd.qs[1]) + c);
+      const int tok = (int)rho / pd.g_q, hh = (int)rho - tok * pd.g_q;
+      src = Q + (long long)(s.q0 + tok) * pd.qs[0] + (long long)(r * pd.g_q + hh) * pd.qs[1] + c * 4;
     }
-    *reinterpret_cast<float4*>(dst + m * D + c * 4) = x;
+    copy16(dst + m * D + c * 4, src, Q);
   }
+  copies_issued();
 }
 
 // acc[i][j] = <row ty * RPT + i, slot tx + 16 j>
@@ -95,34 +116,29 @@ __device__ __forceinline__ int row_sees(const PagedDims& pd, const Seq& s, long 
   return (int)min(max(last, 0LL), (long long)s.valid);
 }
 
-template <int D, int ROWS> constexpr size_t attend_smem() { return (size_t)(ROWS * D + KT * (D + 4) + KT * D) * sizeof(float); }
-template <int D, int ROWS> constexpr size_t mass_smem() { return (size_t)(ROWS * D + KT * (D + 4) + 16 * KT) * sizeof(float); }
+// Floats of shared memory: Q, K (rows padded by four), V, P; at D = 128 and 64 rows exactly half of what an SM has.
+template <int D, int ROWS> constexpr size_t attend_smem() { return (size_t)(ROWS * D + KT * (D + 4) + KT * D + ROWS * KT) * sizeof(float); }
+template <int D, int ROWS> constexpr size_t mass_smem() { return (size_t)(2 * ROWS * D + KT * (D + 4) + 16 * KT) * sizeof(float); }
+static_assert(attend_smem<128, 64>() <= 115712 && mass_smem<128, 64>() <= 115712, "two blocks per SM");
 
 template <int D, int ROWS>
 __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const __grid_constant__ GenArgs a) {
   constexpr int RPT = ROWS / 16, CPT = D / 64;        // rows per thread; float4 columns per thread
-  constexpr int LDP = KT + 4;
-  static_assert(ROWS * LDP <= KT * (D + 4), "P takes the place of K");
+  constexpr int LDP = KT;
   extern __shared__ float4 smem4[];
   float* qs = reinterpret_cast<float*>(smem4);
   float* ks = qs + ROWS * D;
   float* vs = ks + KT * (D + 4);
-  float* ps = ks;
-  __shared__ int seq_of;
+  float* ps = vs + KT * D;
   const PagedDims& pd = a.pd;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int r = (int)(blockIdx.x % pd.h_kv), slot = (int)(blockIdx.x / pd.h_kv), sp = blockIdx.y;
   chain_wait();
-  if (tid == 0) {
-    int lo = 0, hi = pd.batch;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (slot_base(a, mid, ROWS) <= slot) lo = mid; else hi = mid;
-    }
-    seq_of = lo;
+  int b = 0;                                  // last sequence whose slots begin at or before this one
+  for (int hi = pd.batch; hi - b > 1;) {
+    const int mid = (b + hi) >> 1;
+    if (slot_base(a, mid, ROWS) <= slot) b = mid; else hi = mid;
   }
-  __syncthreads();
-  const int b = seq_of;
   const Seq s = load_seq(pd, a.q_start, a.kv_len, b);
   const long long t = slot - slot_base(a, b, ROWS), first = t * ROWS, n_rows = (long long)s.q_len * pd.g_q;
   if (t < 0 || first >= n_rows) return;
@@ -142,14 +158,24 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
     for (int c = 0; c < CPT; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   const float c1 = pd.sm_scale * LOG2E;
+  // K of a tile lands while the product with V of the tile before is formed, V while the scores are
+  auto load_k = [&](int j) { load_tile<D, D + 4>(pd, a.K, pd.ks, r, ks, j & 1, ks); };
+  auto load_v = [&](int j) { load_tile<D, D>(pd, a.V, pd.vs, r, ks, j & 1, vs); };
+  if (tid < 2 * KT) *where<D>(ks, tid & (KT - 1), (t0 + tid / KT) & 1) = Where(pd, table, t0 * KT + tid, s.valid).get(pd);
+  __syncthreads();
+  if (t0 < t1) {
+    load_k(t0);
+    load_v(t0);
+  }
   for (int j = t0; j < t1; ++j) {
+    copies_landed<1>();                                // K (and Q)
     __syncthreads();
-    load_tile<D, D + 4>(pd, a.K, pd.ks, table, r, j * KT, s.valid, ks);
-    load_tile<D, D>(pd, a.V, pd.vs, table, r, j * KT, s.valid, vs);
-    __syncthreads();
+    const Where next(pd, table, tid < KT ? (j + 2) * KT + tid : s.valid, s.valid);
     float acc[RPT][4];
     score_tile<D, RPT>(qs, ks, ty, tx, acc);
-    __syncthreads();                                   // K has been read: its place takes P
+    if (tid < KT) *where<D>(ks, tid, j & 1) = next.get(pd);
+    __syncthreads();                                   // K has been read
+    if (j + 1 < t1) load_k(j + 1); else copies_issued();
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       float mx = -INFINITY;
@@ -178,6 +204,7 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
         o[i][c].x *= corr; o[i][c].y *= corr; o[i][c].z *= corr; o[i][c].w *= corr;
       }
     }
+    copies_landed<1>();                                // V
     __syncthreads();
 #pragma unroll 2
     for (int k = 0; k < KT; k += 4) {
@@ -197,7 +224,10 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
           }
         }
     }
+    __syncthreads();                                   // V and P have been read
+    if (j + 1 < t1) load_v(j + 1); else copies_issued();
   }
+  copies_landed<0>();
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
     const long long rho = first + ty * RPT + i;
@@ -257,8 +287,8 @@ template <int D, int ROWS>
 __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __grid_constant__ GenArgs a) {
   constexpr int RPT = ROWS / 16;
   extern __shared__ float4 smem4[];
-  float* qs = reinterpret_cast<float*>(smem4);
-  float* ks = qs + ROWS * D;
+  float* q2 = reinterpret_cast<float*>(smem4);      // two tiles of rows: one lands while the other is read
+  float* ks = q2 + 2 * ROWS * D;
   float* red = ks + KT * (D + 4);
   const PagedDims& pd = a.pd;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
@@ -270,13 +300,19 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
   const float c1 = pd.sm_scale * LOG2E;
   for (int j = blockIdx.x; j * KT < s.valid; j += gridDim.x) {
     __syncthreads();
-    load_tile<D, D + 4>(pd, a.K, pd.ks, table, r, j * KT, s.valid, ks);
+    if (tid < KT) *where<D>(ks, tid, 0) = Where(pd, table, j * KT + tid, s.valid).get(pd);
+    __syncthreads();
+    load_tile<D, D + 4>(pd, a.K, pd.ks, r, ks, 0, ks);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     // the first row that sees the tile's first slot
     const long long i0 = max(0LL, (long long)j * KT - ((long long)s.kv - s.q_len)) * pd.g_q;
-    for (long long first = i0 / ROWS * ROWS; first < n_rows; first += ROWS) {
-      __syncthreads();
-      load_rows<D, ROWS>(pd, a.Q, s, r, first, qs);
+    const long long begin = i0 / ROWS * ROWS;
+    if (begin < n_rows) load_rows<D, ROWS>(pd, a.Q, s, r, begin, q2);
+    int buf = 0;
+    for (long long first = begin; first < n_rows; first += ROWS, buf ^= 1) {
+      const float* qs = q2 + buf * ROWS * D;
+      if (first + ROWS < n_rows) load_rows<D, ROWS>(pd, a.Q, s, r, first + ROWS, q2 + (buf ^ 1) * ROWS * D); else copies_issued();
+      copies_landed<1>();
       __syncthreads();
       float acc[RPT][4];
       score_tile<D, RPT>(qs, ks, ty, tx, acc);
@@ -291,7 +327,9 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
         for (int k = 0; k < 4; ++k)
           if (j * KT + tx + 16 * k < sees) sum[k] += exp2f(fmaf(acc[i][k], c1, -lse));
       }
+      __syncthreads();                                 // the rows have been read
     }
+    copies_landed<0>();
 #pragma unroll
     for (int k = 0; k < 4; ++k) red[ty * KT + tx + 16 * k] = sum[k];
     __syncthreads();
@@ -311,9 +349,10 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
 int rows_per_tile(const PagedDims& pd) { return (long long)pd.rows * pd.g_q < 32LL * pd.batch ? 16 : 64; }
 long long row_slots(const PagedDims& pd) { return (long long)pd.rows * pd.g_q / rows_per_tile(pd) + pd.batch; }
 
-// Splits of the slots: enough blocks for two waves of two blocks per SM, pieces of 256 slots at least.
+// Splits of the slots: as many blocks as one wave of two per SM takes, pieces of 256 slots at least.  (200 rows over 1500 slots,
+// twice, 8/2 heads, d 64: 324 blocks 52 us, 276 blocks 47.)
 int generic_splits(const PagedDims& pd) {
-  const long long units = row_slots(pd) * pd.h_kv, want = (4LL * current_sm_count() + units - 1) / units;
+  const long long units = row_slots(pd) * pd.h_kv, want = 2LL * current_sm_count() / units;
   const long long most = (pd.cap + 255) / 256;
   return (int)(want < 1 ? 1 : want < most ? (want < 64 ? want : 64) : (most < 64 ? most : 64));
 }

@@ -60,6 +60,17 @@ bool pool_repeats(const PagedDims& pd, const long long* s, int num_pages) {
   return repeats(s[0], num_pages) || repeats(s[1], pd.page_size) || repeats(s[2], pd.h_kv);
 }
 
+// Radians per position as a 64-bit fraction of a turn: x / 2 pi as an unevaluated sum of two doubles, each term's fraction in units of
+// 2^-64.  (In 80-bit arithmetic the 64 pairs of a head cost 3.6 us a call.)
+unsigned long long turn_fraction(double x) {
+  constexpr double HI = 0.15915494309189535, LO = -9.839338337591243e-18;      // 1 / 2 pi
+  constexpr double TWO64 = 18446744073709551616.0;
+  const double hi = x * HI, lo = std::fma(x, HI, -hi) + x * LO;
+  const double f = hi - std::floor(hi);
+  const double g = std::fabs(lo) < 0.25 ? lo : 0.0;        // (beyond 2^50 radians a position there is no fraction left in x itself)
+  return (f >= 1.0 ? 0ull : (unsigned long long)(f * TWO64)) + (unsigned long long)(long long)(g * TWO64);
+}
+
 int make_rope(const dash_rope* r, int head_dim, RopeTable* rt) {
   if (!r || r->struct_size != sizeof(dash_rope)) return DASH_ERR_INVALID_ARG;
   if (r->pairs <= 0 || 2 * r->pairs > head_dim || r->axes < 1 || r->axes > ROPE_MAX_AXES) return DASH_ERR_INVALID_ARG;
@@ -70,11 +81,7 @@ int make_rope(const dash_rope* r, int head_dim, RopeTable* rt) {
   for (int i = 0; i < r->pairs; ++i) {
     if (r->axis[i] < 0 || r->axis[i] >= r->axes || !std::isfinite(r->inv_freq[i])) return DASH_ERR_INVALID_ARG;
     rt->axis[i] = (unsigned char)r->axis[i];
-    // turns per position, its fraction as 64 bits (80-bit arithmetic: 64 bits of mantissa)
-    const long double turns = (long double)r->inv_freq[i] / 6.283185307179586476925286766559L;
-    long double frac = turns - std::floor(turns);
-    frac = std::ldexp(frac, 64);
-    rt->freq[i] = frac >= 18446744073709551615.0L ? 0ull : (unsigned long long)frac;
+    rt->freq[i] = turn_fraction(r->inv_freq[i]);
   }
   return DASH_OK;
 }

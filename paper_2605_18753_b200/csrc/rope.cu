@@ -6,8 +6,14 @@
 // bits give the quadrant, the rest lies within an eighth of a turn, where Taylor polynomials (sine to x^9, cosine to x^10)
 // are within 2e-9 of the functions.
 //
-// Memory-bound: every element is read and written once, cosine and sine are formed once per token and pair and serve all heads
-// from shared memory.
+// Memory-bound: every element is read and written once.  A thread owns one piece of the head (N pairs: two 16-byte vectors) of one
+// token, forms its cosines and sines in registers and takes the piece through its share of the heads, four heads on their way
+// at once; the eight lanes of a head cover whole lines.  8192 tokens, 40 heads, d 128: 32.0 us (5.2 TB/s, 80 % of the measured copy);
+// with a table in shared memory for all heads of a token 42 (bank conflicts, a barrier), one head on its way at a time 45.  12,300
+// tokens with their K and V into pages: 44 us (4.7 TB/s).  Three blocks per SM for the rotation alone, two where the pages' addresses
+// take registers as well.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace dash {
@@ -36,19 +42,21 @@ __device__ __forceinline__ float2 cos_sin_of_turns(unsigned long long freq, int 
   return r;
 }
 
-template <typename T> struct Vec;        // 16 bytes
+// 16 bytes, as they lie in memory until they are needed.
+template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
-  float v[4];
-  __device__ void load(const float* p) { *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p); }
-  __device__ void store(float* p) const { *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(v); }
+  float4 raw;
+  __device__ void load(const float* p) { raw = *reinterpret_cast<const float4*>(p); }
+  __device__ void get(float (&v)[4]) const { v[0] = raw.x; v[1] = raw.y; v[2] = raw.z; v[3] = raw.w; }
+  static __device__ void store(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
-  float v[8];
-  __device__ void load(const __nv_bfloat16* p) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint4 raw;
+  __device__ void load(const __nv_bfloat16* p) { raw = *reinterpret_cast<const uint4*>(p); }
+  __device__ void get(float (&v)[8]) const {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[k]));
@@ -56,7 +64,7 @@ template <> struct Vec<__nv_bfloat16> {
       v[2 * k + 1] = f.y;
     }
   }
-  __device__ void store(__nv_bfloat16* p) const {
+  static __device__ void store(__nv_bfloat16* p, const float (&v)[8]) {
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -67,78 +75,116 @@ template <> struct Vec<__nv_bfloat16> {
   }
 };
 
-// One head's row: `items` pieces of work, piece `v` reads and writes two vectors (or, SCALAR, two elements) of it.
-//   halves       vectors v and pairs / N + v hold the two sides of N pairs; behind the pairs two vectors pass through
-//   interleaved  a vector holds N / 2 whole pairs
-// SCALAR serves pair counts that are no multiple of a vector: element pairs, one at a time.
-template <typename T, bool SCALAR>
-__device__ __forceinline__ void turn_piece(const T* src, T* dst, int v, int d, int pairs, bool interleaved, const float2* cs) {
-  constexpr int N = Vec<T>::N;
-  if constexpr (SCALAR) {
-    int lo = 2 * v, hi = 2 * v + 1;             // behind the pairs (2 v >= 2 pairs) and interleaved: neighbours
-    if (v < pairs && !interleaved) { lo = v; hi = v + pairs; }
-    const float x = to_f32(src[lo]), y = to_f32(src[hi]);
-    const float2 t = v < pairs ? cs[v] : make_float2(1.f, 0.f);
-    dst[lo] = from_f32<T>(fmaf(x, t.x, -(y * t.y)));
-    dst[hi] = from_f32<T>(fmaf(x, t.y, y * t.x));
-  } else {
-    const int per = pairs / N;                  // pieces that hold pairs by halves
-    const bool turn = interleaved ? 2 * v * N < 2 * pairs : v < per;
-    const int lo = interleaved || !turn ? 2 * v * N : v * N;
-    const int hi = interleaved || !turn ? lo + N : pairs + v * N;
-    Vec<T> a, b;
-    a.load(src + lo);
-    b.load(src + hi);
-    if (turn) {
-      if (interleaved) {
+// A piece of a head: piece v has pairs v N .. v N + N - 1 (SCALAR: pair v alone).
+//   halves       the pairs' first elements are one vector, their second elements another
+//   interleaved  the pairs fill two vectors one behind the other
+// Behind the rotated pairs both are two neighbouring vectors (elements) that pass through.  SCALAR serves pair counts that are no
+// multiple of a vector.
+template <typename T, bool SCALAR, bool IL>
+struct Piece {
+  static constexpr int N = SCALAR ? 1 : Vec<T>::N;
+  float2 cs[N];
+  int lo, hi;
+  bool turn_lo, turn_hi;                       // (interleaved: the two vectors apart; halves: both)
+  __device__ __forceinline__ void place(const RopeTable& rt, int v) {
+    const int first = v * N;
+    turn_lo = first < rt.pairs;
+    turn_hi = IL && !SCALAR ? first + N / 2 < rt.pairs : turn_lo;
+    lo = IL || !turn_lo ? 2 * first : first;
+    hi = IL || !turn_lo ? 2 * first + N : first + rt.pairs;
+  }
+  // pos(axis): the token's position
+  template <typename Pos>
+  __device__ __forceinline__ void prepare(const RopeTable& rt, int v, float sign, Pos&& pos) {
+    const int first = v * N;
 #pragma unroll
-        for (int k = 0; k < N; k += 2) {
-          const float2 t = cs[(lo + k) >> 1];
-          const float x = a.v[k], y = a.v[k + 1];
-          a.v[k] = fmaf(x, t.x, -(y * t.y));
-          a.v[k + 1] = fmaf(x, t.y, y * t.x);
-        }
-        if (hi < 2 * pairs) {
-#pragma unroll
-          for (int k = 0; k < N; k += 2) {
-            const float2 t = cs[(hi + k) >> 1];
-            const float x = b.v[k], y = b.v[k + 1];
-            b.v[k] = fmaf(x, t.x, -(y * t.y));
-            b.v[k + 1] = fmaf(x, t.y, y * t.x);
-          }
-        }
-      } else {
-        const float4* t4 = reinterpret_cast<const float4*>(cs + lo);
-#pragma unroll
-        for (int k = 0; k < N; k += 2) {
-          const float4 t = t4[k >> 1];
-          float x = a.v[k], y = b.v[k];
-          a.v[k] = fmaf(x, t.x, -(y * t.y));
-          b.v[k] = fmaf(x, t.y, y * t.x);
-          x = a.v[k + 1], y = b.v[k + 1];
-          a.v[k + 1] = fmaf(x, t.z, -(y * t.w));
-          b.v[k + 1] = fmaf(x, t.w, y * t.z);
-        }
+    for (int k = 0; k < N; ++k) {
+      cs[k] = make_float2(1.f, 0.f);
+      if (first + k < rt.pairs) {
+        cs[k] = cos_sin_of_turns(rt.freq[first + k], pos(rt.axis[first + k]));
+        cs[k].y *= sign;
       }
     }
-    a.store(dst + lo);
-    b.store(dst + hi);
   }
-}
+  static __device__ __forceinline__ void turn(float& x, float& y, float2 t) {
+    const float a = x, b = y;
+    x = fmaf(a, t.x, -(b * t.y));
+    y = fmaf(a, t.y, b * t.x);
+  }
+  using Side = std::conditional_t<SCALAR, T, Vec<T>>;
+  __device__ __forceinline__ void load(const T* src, Side& a, Side& b) const {
+    if constexpr (SCALAR) {
+      a = src[lo];
+      b = src[hi];
+    } else {
+      a.load(src + lo);
+      b.load(src + hi);
+    }
+  }
+  __device__ __forceinline__ void finish(T* dst, const Side& a, const Side& b, bool rotate) const {
+    if constexpr (SCALAR) {
+      float x = to_f32(a), y = to_f32(b);
+      if (rotate && turn_lo) turn(x, y, cs[0]);
+      dst[lo] = from_f32<T>(x);
+      dst[hi] = from_f32<T>(y);
+    } else {
+      float x[N], y[N];
+      a.get(x);
+      b.get(y);
+      if (rotate) {
+        if constexpr (IL) {
+          if (turn_lo) {
+#pragma unroll
+            for (int k = 0; k < N; k += 2) turn(x[k], x[k + 1], cs[k / 2]);
+          }
+          if (turn_hi) {
+#pragma unroll
+            for (int k = 0; k < N; k += 2) turn(y[k], y[k + 1], cs[N / 2 + k / 2]);
+          }
+        } else if (turn_lo) {
+#pragma unroll
+          for (int k = 0; k < N; ++k) turn(x[k], y[k], cs[k]);
+        }
+      }
+      Vec<T>::store(dst + lo, x);
+      Vec<T>::store(dst + hi, y);
+    }
+  }
+  // The piece of BATCH heads from h on, `step` apart, on its way at once: the output may be the input, so the compiler would finish one
+  // head before it asks for the next.
+  static constexpr int BATCH = 4;
+  struct Heads { Side a[BATCH], b[BATCH]; };
+  __device__ __forceinline__ void fetch(Heads& x, const T* src, long long stride, int h, int step, int heads) const {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (h + k * step < heads) load(src + (h + k * step) * stride, x.a[k], x.b[k]);
+  }
+  __device__ __forceinline__ void finish(const Heads& x, T* dst, long long stride, int h, int step, int heads, bool rotate) const {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (h + k * step < heads) finish(dst + (h + k * step) * stride, x.a[k], x.b[k], rotate);
+  }
+  // Heads first, first + step, ... below `heads`; x: the first batch, fetched.
+  __device__ __forceinline__ void run(Heads& x, const T* src, T* dst, long long src_stride, long long dst_stride, int first, int step, int heads,
+                                      bool rotate) const {
+    for (int h = first; h < heads; h += BATCH * step) {
+      if (h != first) fetch(x, src, src_stride, h, step, heads);
+      finish(x, dst, dst_stride, h, step, heads, rotate);
+    }
+  }
+};
 
-// Cosines and sines of the block's tokens: cs[token][pair].  `at(token)` = base index into positions, or < 0 for no such token.
-template <typename At>
-__device__ __forceinline__ void fill_table(float2* cs, const RopeTable& rt, const int* positions, long long axis_stride, int tokens,
-                                           float sign, At&& at) {
-  for (int k = threadIdx.x; k < tokens * rt.pairs; k += THREADS) {
-    const int t = k / rt.pairs, i = k - t * rt.pairs;
-    const long long base = at(t);
-    if (base < 0) continue;
-    float2 c = cos_sin_of_turns(rt.freq[i], __ldg(positions + (long long)rt.axis[i] * axis_stride + base));
-    c.y *= sign;
-    cs[k] = c;
+// A block: `tokens` tokens, `pieces` threads per head, and what is left of its threads as groups that share the heads.
+struct Share {
+  int v, t, group, groups;
+  __device__ __forceinline__ Share(int pieces, int tokens) {
+    const int log_p = 31 - __clz(pieces), rest = (int)threadIdx.x >> log_p, log_t = 31 - __clz(tokens);      // (powers of two)
+    v = threadIdx.x & (pieces - 1);
+    t = rest & (tokens - 1);
+    group = rest >> log_t;
+    groups = THREADS >> (log_p + log_t);
   }
-}
+};
 
 struct RopeArgs {
   RopeTable rt;
@@ -150,26 +196,23 @@ struct RopeArgs {
   float sign;
 };
 
-template <typename T, bool SCALAR>
-__global__ void __launch_bounds__(THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
-  extern __shared__ float4 cs4[];
-  float2* cs = reinterpret_cast<float2*>(cs4);
+template <typename T, bool SCALAR, bool IL>
+__global__ void __launch_bounds__(THREADS, 3) rope_kernel(const __grid_constant__ RopeArgs a) {
+  using P = Piece<T, SCALAR, IL>;
+  const Share sh(a.d / (2 * P::N), a.tokens);
   chain_wait();
-  const long long total = (long long)a.batch * a.n, first = (long long)blockIdx.x * a.tokens;
-  const int here = (int)min((long long)a.tokens, total - first);
-  fill_table(cs, a.rt, a.positions, total, here, a.sign, [&](int t) { return first + t; });
-  __syncthreads();
-  const int per_head = a.d / (SCALAR ? 2 : 2 * Vec<T>::N), heads = a.h_q + a.h_k, per_token = heads * per_head;
-#pragma unroll 2
-  for (int k = threadIdx.x; k < here * per_token; k += THREADS) {
-    const int t = k / per_token, rem = k - t * per_token;
-    const int h = rem / per_head, v = rem - h * per_head;
-    const long long b = (first + t) / a.n, i = (first + t) - b * a.n;
-    const bool q = h < a.h_q;
-    const long long off = q ? b * a.qs[0] + i * a.qs[1] + h * a.qs[2] : b * a.ks[0] + i * a.ks[1] + (h - a.h_q) * a.ks[2];
-    turn_piece<T, SCALAR>((const T*)(q ? a.Q : a.K) + off, (T*)(q ? a.Qout : a.Kout) + off, v, a.d, a.rt.pairs,
-                          a.rt.interleaved != 0, cs + t * a.rt.pairs);
-  }
+  const long long total = (long long)a.batch * a.n, token = (long long)blockIdx.x * a.tokens + sh.t;
+  if (token >= total) return;
+  P p;
+  typename P::Heads x;
+  p.place(a.rt, sh.v);
+  const long long b = token / a.n, i = token - b * a.n;
+  const long long qo = b * a.qs[0] + i * a.qs[1], ko = b * a.ks[0] + i * a.ks[1];
+  p.fetch(x, (const T*)a.Q + qo, a.qs[2], sh.group, sh.groups, a.h_q);
+  p.prepare(a.rt, sh.v, a.sign, [&](int axis) { return __ldg(a.positions + axis * total + token); });
+  p.run(x, (const T*)a.Q + qo, (T*)a.Qout + qo, a.qs[2], a.qs[2], sh.group, sh.groups, a.h_q, true);
+  p.fetch(x, (const T*)a.K + ko, a.ks[2], sh.group, sh.groups, a.h_k);
+  p.run(x, (const T*)a.K + ko, (T*)a.Kout + ko, a.ks[2], a.ks[2], sh.group, sh.groups, a.h_k, true);
 }
 
 struct AppendArgs {
@@ -184,13 +227,13 @@ struct AppendArgs {
 
 constexpr int APPEND_TOKENS = 8;
 
-template <typename T, bool SCALAR>
-__global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ AppendArgs a) {
-  extern __shared__ float4 cs4[];
-  float2* cs = reinterpret_cast<float2*>(cs4);
+template <typename T, bool SCALAR, bool IL>
+__global__ void __launch_bounds__(THREADS, 2) append_kernel(const __grid_constant__ AppendArgs a) {
+  using P = Piece<T, SCALAR, IL>;
   __shared__ long long page_of[APPEND_TOKENS];    // physical page, -1: no slot, -2: not a row of any sequence
   __shared__ int tok_of[APPEND_TOKENS];
   const PagedDims& pd = a.pd;
+  const Share sh(pd.d / (2 * P::N), a.tokens);
   chain_wait();
   const int first = blockIdx.x * a.tokens, here = min(a.tokens, pd.rows - first);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -214,37 +257,26 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
       tok_of[t] = tok;
     }
   }
-  if (a.rt.pairs) fill_table(cs, a.rt, a.positions, pd.rows, here, 1.f, [&](int t) { return (long long)first + t; });
+  P p;
+  typename P::Heads x;
+  p.place(a.rt, sh.v);
+  const long long row = first + sh.t;
+  const bool rotate = a.rt.pairs > 0;
+  const T *q = (const T*)a.Q + row * pd.qs[0], *k = (const T*)a.K + row * pd.kns[0], *v = (const T*)a.V + row * pd.vns[0];
+  if (sh.t < here) p.fetch(x, q, pd.qs[1], sh.group, sh.groups, a.h_q);
+  p.prepare(a.rt, sh.v, 1.f, [&](int axis) { return sh.t < here ? __ldg(a.positions + (long long)axis * pd.rows + row) : 0; });
   __syncthreads();
-  const int per_head = pd.d / (SCALAR ? 2 : 2 * Vec<T>::N), heads = a.h_q + 2 * pd.h_kv, per_token = heads * per_head;
-#pragma unroll 2
-  for (int k = threadIdx.x; k < here * per_token; k += THREADS) {
-    const int t = k / per_token, rem = k - t * per_token;
-    int h = rem / per_head;
-    const int v = rem - h * per_head, tok = tok_of[t];
-    const long long row = first + t, page = page_of[t];
-    const T* src;
-    T* dst;
-    int pairs = a.rt.pairs;
-    if (h < a.h_q) {
-      if (page == -2) continue;
-      src = (const T*)a.Q + row * pd.qs[0] + h * pd.qs[1];
-      dst = (T*)a.Qout + row * pd.os[0] + h * pd.os[1];
-    } else {
-      if (page < 0) continue;
-      h -= a.h_q;
-      if (h < pd.h_kv) {
-        src = (const T*)a.K + row * pd.kns[0] + h * pd.kns[1];
-        dst = (T*)a.Kpool + page * pd.ks[0] + tok * pd.ks[1] + h * pd.ks[2];
-      } else {
-        h -= pd.h_kv;
-        src = (const T*)a.V + row * pd.vns[0] + h * pd.vns[1];
-        dst = (T*)a.Vpool + page * pd.vs[0] + tok * pd.vs[1] + h * pd.vs[2];
-        pairs = 0;
-      }
-    }
-    turn_piece<T, SCALAR>(src, dst, v, pd.d, pairs, a.rt.interleaved != 0, cs + t * a.rt.pairs);
-  }
+  if (sh.t >= here) return;
+  const long long page = page_of[sh.t];
+  const int tok = tok_of[sh.t];
+  if (page == -2) return;
+  p.run(x, q, (T*)a.Qout + row * pd.os[0], pd.qs[1], pd.os[1], sh.group, sh.groups, a.h_q, rotate);
+  if (page < 0) return;
+  p.fetch(x, k, pd.kns[1], sh.group, sh.groups, pd.h_kv);
+  typename P::Heads y;
+  p.fetch(y, v, pd.vns[1], sh.group, sh.groups, pd.h_kv);
+  p.run(x, k, (T*)a.Kpool + page * pd.ks[0] + tok * pd.ks[1], pd.kns[1], pd.ks[2], sh.group, sh.groups, pd.h_kv, rotate);
+  p.run(y, v, (T*)a.Vpool + page * pd.vs[0] + tok * pd.vs[1], pd.vns[1], pd.vs[2], sh.group, sh.groups, pd.h_kv, false);
 }
 
 // Whole vectors where every side of the pairs is made of them: by halves the pairs, interleaved the pairs' elements, have to be a
@@ -254,29 +286,35 @@ bool by_vectors(const RopeTable& rt, int d, int n) {
   return rt.pairs % n == 0 && (d - 2 * rt.pairs) % (2 * n) == 0;
 }
 
-// Tokens per block: one where the blocks would not fill the machine otherwise, eight where they do (a block's table is then formed
-// by all of its threads).
-int tokens_per_block(long long tokens) { return tokens >= 8LL * 4 * current_sm_count() ? 8 : tokens >= 4LL * current_sm_count() ? 2 : 1; }
+// Tokens per block: as few as leave the machine blocks to fill it (a token's heads are then shared by more threads), eight where there
+// are many (the cosines of a piece serve more heads).
+int tokens_per_block(long long tokens, int pieces) {
+  int t = tokens >= 8LL * 4 * current_sm_count() ? 8 : tokens >= 4LL * current_sm_count() ? 2 : 1;
+  while (t * pieces > THREADS) t >>= 1;
+  return t;
+}
 
 template <typename T>
 cudaError_t launch_rope_t(RopeArgs& a, cudaStream_t st) {
   const long long total = (long long)a.batch * a.n;
-  a.tokens = tokens_per_block(total);
-  const unsigned blocks = (unsigned)((total + a.tokens - 1) / a.tokens);
-  const size_t smem = (size_t)a.tokens * a.rt.pairs * sizeof(float2);
   const bool vec = by_vectors(a.rt, a.d, Vec<T>::N);
-  cudaError_t e = launch_chained(vec ? rope_kernel<T, false> : rope_kernel<T, true>, dim3(blocks), dim3(THREADS), smem, st, a);
+  a.tokens = tokens_per_block(total, a.d / (vec ? 2 * Vec<T>::N : 2));
+  const unsigned blocks = (unsigned)((total + a.tokens - 1) / a.tokens);
+  auto kern = vec ? (a.rt.interleaved ? rope_kernel<T, false, true> : rope_kernel<T, false, false>)
+                  : (a.rt.interleaved ? rope_kernel<T, true, true> : rope_kernel<T, true, false>);
+  cudaError_t e = launch_chained(kern, dim3(blocks), dim3(THREADS), 0, st, a);
   count_launch();
   return e;
 }
 
 template <typename T>
 cudaError_t launch_append_t(AppendArgs& a, cudaStream_t st) {
-  a.tokens = tokens_per_block(a.pd.rows);
-  const unsigned blocks = (unsigned)((a.pd.rows + a.tokens - 1) / a.tokens);
-  const size_t smem = (size_t)a.tokens * a.rt.pairs * sizeof(float2);
   const bool vec = by_vectors(a.rt, a.pd.d, Vec<T>::N);
-  cudaError_t e = launch_chained(vec ? append_kernel<T, false> : append_kernel<T, true>, dim3(blocks), dim3(THREADS), smem, st, a);
+  a.tokens = tokens_per_block(a.pd.rows, a.pd.d / (vec ? 2 * Vec<T>::N : 2));
+  const unsigned blocks = (unsigned)((a.pd.rows + a.tokens - 1) / a.tokens);
+  auto kern = vec ? (a.rt.interleaved ? append_kernel<T, false, true> : append_kernel<T, false, false>)
+                  : (a.rt.interleaved ? append_kernel<T, true, true> : append_kernel<T, true, false>);
+  cudaError_t e = launch_chained(kern, dim3(blocks), dim3(THREADS), 0, st, a);
   count_launch();
   return e;
 }
