@@ -428,77 +428,68 @@ def params_for_paged(Kpool, Vpool, page_table, *, h_q, rows=None, Q=None, O=None
 
 
 _I32, _F32 = torch.int32, torch.float32
+_TORCH_DTYPE = (torch.float32, torch.bfloat16)        # by dash_dtype
 
 
-def _bad(where, t, kind):
-    raise ValueError(f"{where}: expected a contiguous {kind} tensor on the current device, got {t.dtype} on {t.device}, strides {t.stride()}")
+def _refuse(where, dtype, ints, floats, tensors):
+    """Says which argument the kernels would misread: they take index tensors as contiguous int32, lse and mass as contiguous fp32,
+    queries, keys and values in the parameters' dtype, all on the current device."""
+    for kind, want, ts in (("int32", _I32, ints), ("float32", _F32, floats), ("", dtype, tensors)):
+        for t in ts:
+            if t is None:
+                continue
+            if t.dtype is not want or (kind and not t.is_contiguous()) or t.get_device() != torch._C._cuda_getDevice():
+                raise ValueError(f"{where}: expected a {'contiguous ' if kind else ''}{want} tensor on the current device, got {t.dtype} "
+                                 f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-# The kernels read index tensors as contiguous int32, lse and mass as contiguous fp32, on the current device; anything else would be
-# misread in silence.  (One walk over the arguments gives the addresses as well: 1.5 us of a call's 5.)
-def _i32(where, dev, *ts):
-    out = []
-    for t in ts:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not _I32 or t.get_device() != dev or not t.is_contiguous():
-            _bad(where, t, "int32")
-        out.append(t.data_ptr())
-    return out
-
-
-def _f32(where, dev, *ts):
-    out = []
-    for t in ts:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not _F32 or t.get_device() != dev or not t.is_contiguous():
-            _bad(where, t, "float32")
-        out.append(t.data_ptr())
-    return out
-
-
-def _of(where, dev, dtype, *ts):
-    """Addresses of tensors of queries, keys and values: the parameters' dtype, on the current device."""
-    out = []
-    for t in ts:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not dtype or t.get_device() != dev:
-            raise ValueError(f"{where}: expected {dtype} on the current device, got {t.dtype} on {t.device}")
-        out.append(t.data_ptr())
-    return out
-
-
-_TORCH_DTYPE = {DASH_F32: torch.float32, DASH_BF16: torch.bfloat16}
-
+# A short call is a kernel of a few microseconds, so what these checks cost counts: one expression on the way that is taken, the search
+# for the culprit only behind it.
 
 def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
     """Q and K (either may be None) of a prefill shape rotated; inverse=True turns them back, which is the backward pass when it is
     given the gradients.  positions int32 [axes, batch, seq]; outputs have the strides of their inputs and may be them."""
-    dev = torch._C._cuda_getDevice()
-    pos, = _i32("dash_attn_rope", dev, positions)
-    q, k, qo, ko = _of("dash_attn_rope", dev, _TORCH_DTYPE[p.dtype], Q, K, Qout, Kout)
+    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    if not (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()):
+        _refuse("dash_attn_rope", dt, (positions,), (), ())
+    for x, y in ((Q, Qout), (K, Kout)):
+        if x is None and y is None:
+            continue
+        if x is None or y is None:
+            raise ValueError("dash_attn_rope: every input has an output")
+        if not (x.dtype is dt and y.dtype is dt and x.get_device() == dev and y.get_device() == dev):
+            _refuse("dash_attn_rope", dt, (), (), (x, y))
+        if x is not y and not (x.is_contiguous() and y.is_contiguous()) and x.stride() != y.stride():
+            raise ValueError("dash_attn_rope: an output has the strides of its input")
     if positions.numel() != rope.axes * p.batch * p.seq_q:
         raise ValueError("positions must be [axes, batch, seq]")
-    if (Q is not None and Qout is not None and Q.stride() != Qout.stride()) or (K is not None and Kout is not None and K.stride() != Kout.stride()):
-        raise ValueError("dash_attn_rope: an output has the strides of its input")
-    _check(lib().dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), pos, q, k, qo, ko, int(inverse), _stream()), "dash_attn_rope")
+    rc = (_lib or lib()).dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), positions.data_ptr(), Q if Q is None else Q.data_ptr(),
+                                        K if K is None else K.data_ptr(), Q if Q is None else Qout.data_ptr(),
+                                        K if K is None else Kout.data_ptr(), 1 if inverse else 0, torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise DashError(rc, "dash_attn_rope")
 
 
 def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Qout, K, V, Kpool, Vpool):
     """Packed new tokens into their pages: K rotated, V as it is, Q rotated into Qout (Q and Qout None: keys and values only;
     rope and positions None: no rotation)."""
-    dev = torch._C._cuda_getDevice()
-    pos, qs, kl, table = _i32("dash_attn_append_paged", dev, positions, q_start, kv_len, page_table)
-    q, qo, k, v, kp, vp = _of("dash_attn_append_paged", dev, _TORCH_DTYPE[p.dtype], Q, Qout, K, V, Kpool, Vpool)
+    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and K.dtype is dt and V.dtype is dt
+            and Kpool.dtype is dt and Vpool.dtype is dt and q_start.get_device() == dev and kv_len.get_device() == dev
+            and page_table.get_device() == dev and K.get_device() == dev and V.get_device() == dev and Kpool.get_device() == dev
+            and Vpool.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
+            and (positions is None or (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()))
+            and (Q is None or (Q.dtype is dt and Q.get_device() == dev)) and (Qout is None or (Qout.dtype is dt and Qout.get_device() == dev))):
+        _refuse("dash_attn_append_paged", dt, (positions, q_start, kv_len, page_table), (), (Q, Qout, K, V, Kpool, Vpool))
     if positions is not None and positions.numel() != rope.axes * p.rows:
         raise ValueError("positions must be [axes, rows]")
-    _check(lib().dash_attn_append_paged(ctypes.byref(p), None if rope is None else ctypes.byref(rope), pos, qs, kl, table, q, qo, k, v,
-                                        kp, vp, _stream()), "dash_attn_append_paged")
+    rc = (_lib or lib()).dash_attn_append_paged(
+        ctypes.byref(p), None if rope is None else ctypes.byref(rope), None if positions is None else positions.data_ptr(),
+        q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), None if Q is None else Q.data_ptr(),
+        None if Qout is None else Qout.data_ptr(), K.data_ptr(), V.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(),
+        torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise DashError(rc, "dash_attn_append_paged")
 
 
 def dash_attn_paged_workspace_bytes(p: DashPagedParams) -> int:
@@ -517,36 +508,62 @@ def alloc_paged_workspace(p: DashPagedParams, device="cuda") -> torch.Tensor:
 
 def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len, O, lse, workspace):
     """Dense causal attention of packed new tokens over their sequences' pages; lse (None to skip) fp32 [rows, h_q]."""
-    dev = torch._C._cuda_getDevice()
-    table, qs, kl = _i32("dash_attn_attend_chunk_paged", dev, page_table, q_start, kv_len)
-    ls, = _f32("dash_attn_attend_chunk_paged", dev, lse)
-    q, kp, vp, o = _of("dash_attn_attend_chunk_paged", dev, _TORCH_DTYPE[p.dtype], Q, Kpool, Vpool, O)
-    _check(lib().dash_attn_attend_chunk_paged(ctypes.byref(p), q, kp, vp, table, qs, kl, o, ls, workspace.data_ptr(), workspace.numel(),
-                                              _stream()), "dash_attn_attend_chunk_paged")
+    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and Q.dtype is dt and O.dtype is dt
+            and Kpool.dtype is dt and Vpool.dtype is dt and q_start.get_device() == dev and kv_len.get_device() == dev
+            and page_table.get_device() == dev and Q.get_device() == dev and O.get_device() == dev and Kpool.get_device() == dev
+            and Vpool.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
+            and (lse is None or (lse.dtype is _F32 and lse.get_device() == dev and lse.is_contiguous()))):
+        _refuse("dash_attn_attend_chunk_paged", dt, (page_table, q_start, kv_len), (lse,), (Q, Kpool, Vpool, O))
+    rc = (_lib or lib()).dash_attn_attend_chunk_paged(
+        ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
+        O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise DashError(rc, "dash_attn_attend_chunk_paged")
 
 
 def dash_attn_key_mass_paged(p, Q, Kpool, page_table, q_start, kv_len, lse, mass_in, mass_out, workspace, decay=1.0):
     """Weights that the new rows give every cached token, added to decay * mass_in (None: zeros); fp32 [batch, h_kv, slots]."""
-    dev = torch._C._cuda_getDevice()
-    table, qs, kl = _i32("dash_attn_key_mass_paged", dev, page_table, q_start, kv_len)
-    ls, mi, mo = _f32("dash_attn_key_mass_paged", dev, lse, mass_in, mass_out)
-    q, kp = _of("dash_attn_key_mass_paged", dev, _TORCH_DTYPE[p.dtype], Q, Kpool)
-    _check(lib().dash_attn_key_mass_paged(ctypes.byref(p), q, kp, table, qs, kl, ls, decay, mi, mo, workspace.data_ptr(),
-                                          workspace.numel(), _stream()), "dash_attn_key_mass_paged")
+    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and Q.dtype is dt and Kpool.dtype is dt
+            and lse.dtype is _F32 and mass_out.dtype is _F32 and q_start.get_device() == dev and kv_len.get_device() == dev
+            and page_table.get_device() == dev and Q.get_device() == dev and Kpool.get_device() == dev and lse.get_device() == dev
+            and mass_out.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
+            and lse.is_contiguous() and mass_out.is_contiguous()
+            and (mass_in is None or (mass_in.dtype is _F32 and mass_in.get_device() == dev and mass_in.is_contiguous()))):
+        _refuse("dash_attn_key_mass_paged", dt, (page_table, q_start, kv_len), (lse, mass_in, mass_out), (Q, Kpool))
+    rc = (_lib or lib()).dash_attn_key_mass_paged(
+        ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), lse.data_ptr(),
+        decay, None if mass_in is None else mass_in.data_ptr(), mass_out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise DashError(rc, "dash_attn_key_mass_paged")
 
 
 def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_len, dst_table, Kdst, Vdst, mass_out=None, *, keep,
                           sinks=0, recent=0):
     """Keeps `keep` tokens of every (sequence, KV head) and moves them to the front of the destination pages (page_table, Kpool,
     Vpool themselves for in place)."""
-    dev = torch._C._cuda_getDevice()
-    kl, table, kept_at, len_at, dst = _i32("dash_attn_evict_paged", dev, kv_len, page_table, kept, new_len, dst_table)
-    m, mo = _f32("dash_attn_evict_paged", dev, mass, mass_out)
-    kp, vp, kd, vd = _of("dash_attn_evict_paged", dev, _TORCH_DTYPE[p.dtype], Kpool, Vpool, Kdst, Vdst)
-    if Kdst.stride() != Kpool.stride() or Vdst.stride() != Vpool.stride() or Kdst.shape[1:] != Kpool.shape[1:]:
+    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    if not (kv_len.dtype is _I32 and page_table.dtype is _I32 and kept.dtype is _I32 and new_len.dtype is _I32 and dst_table.dtype is _I32
+            and mass.dtype is _F32 and Kpool.dtype is dt and Vpool.dtype is dt and Kdst.dtype is dt and Vdst.dtype is dt
+            and kv_len.get_device() == dev and page_table.get_device() == dev and kept.get_device() == dev and new_len.get_device() == dev
+            and dst_table.get_device() == dev and mass.get_device() == dev and Kpool.get_device() == dev and Vpool.get_device() == dev
+            and Kdst.get_device() == dev and Vdst.get_device() == dev and kv_len.is_contiguous() and page_table.is_contiguous()
+            and kept.is_contiguous() and new_len.is_contiguous() and dst_table.is_contiguous() and mass.is_contiguous()
+            and (mass_out is None or (mass_out.dtype is _F32 and mass_out.get_device() == dev and mass_out.is_contiguous()))):
+        _refuse("dash_attn_evict_paged", dt, (kv_len, page_table, kept, new_len, dst_table), (mass, mass_out), (Kpool, Vpool, Kdst, Vdst))
+    shape = Kdst.shape
+    if shape[1:] != Kpool.shape[1:] or not (Kdst.is_contiguous() and Kpool.is_contiguous() or Kdst.stride() == Kpool.stride()) \
+            or not (Vdst.is_contiguous() and Vpool.is_contiguous() or Vdst.stride() == Vpool.stride()):
         raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' page size, heads and strides")
-    _check(lib().dash_attn_evict_paged(ctypes.byref(p), keep, sinks, recent, m, kl, table, kp, vp, kept_at, len_at, dst, dst_table.shape[1],
-                                       Kdst.shape[0], kd, vd, mo, _stream()), "dash_attn_evict_paged")
+    rc = (_lib or lib()).dash_attn_evict_paged(
+        ctypes.byref(p), keep, sinks, recent, mass.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(),
+        kept.data_ptr(), new_len.data_ptr(), dst_table.data_ptr(), dst_table.shape[1], shape[0], Kdst.data_ptr(), Vdst.data_ptr(),
+        None if mass_out is None else mass_out.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise DashError(rc, "dash_attn_evict_paged")
 
 
 def dash_attn_reset_status(workspace):
