@@ -17,8 +17,17 @@
 // block to arrive instead, inside this kernel: 8 to 14 us of fences, counters and dependent loads at the end of every block.)
 //
 // Warp roles (384 threads): warps 0-3 and 4-7 softmax of stage 0 / 1, a row per thread; warp 8 loads Q and K, warp 9 V (TMA, a box
-// per page or per 128 tokens of one), warp 10 issues the MMAs, warp 11 completes the warpgroup for setmaxnreg.  P is written over S in
-// tensor memory (bf16) and is the A operand of P V.
+// per page or per 128 tokens of one), warps 10 and 11 issue the MMAs of stage 0 / 1 (one warp for both: a wait for one stage's
+// weights held up the other's scores).  P is written over S in tensor memory (bf16) and is the A operand of P V; its first three
+// quarters go to the product while the last is formed.
+//
+// What bounds it: 4096 rows over 16384 slots, 32/8 heads, d 128 (962 GFLOP): 765 us, 1.26 PFLOP/s, 75 % of the measured cuBLAS burst
+// (in a long loop the power limit holds it at 0.89 ms); the same schedule without the softmax arithmetic takes 608 us, without
+// all but one MMA of each product 665, so the softmax threads' chain of a step (scores out of tensor memory, maximum, 128
+// exponentials, weights back) is the longer of the two.  Tried and slower: steps of 64 slots with two score buffers (the scores'
+// products then read Q from shared memory twice as often), two warpgroups per stage (1.18 ms: 96 registers a thread), the weights
+// formed ahead of the maximum.  One token of each of 16 caches of up to 65536 slots (2.4 GB): 378 us, 6.4 TB/s, 97 % of the measured
+// copy.
 // Every wait is bounded; one that runs out raises DASH_ERR_TIMEOUT in the status word, and every role leaves.
 #include <cuda.h>
 
