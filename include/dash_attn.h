@@ -351,7 +351,9 @@ int dash_attn_append_paged(const dash_paged_params* p, const dash_rope* rope, co
  *   o_i = sum_{t <= slot(i)} softmax_t(<q_i, k_t> / sqrt(d)) v_t,     lse_i = log sum_{t <= slot(i)} exp(<q_i, k_t> / sqrt(d)).
  * It serves the layers, and the short contexts, that are not routed, from the cache that dash_attn_fwd_decode_paged reads: one
  * token per sequence, whole prompts, or both in one call.
- *   O    by p->o_stride, dtype p->dtype.  A row without a visible key (a slot below 0) gets 0 and lse -inf.
+ *   O    by p->o_stride, dtype p->dtype.  A row without a visible key (a slot below 0) gets 0 and lse -inf; a NaN in a query,
+ *        or in a key that the row sees, makes the row NaN in both, and no row that does not see it.  Cached values are taken to be
+ *        finite (0 times a NaN of a token that the row does not see yet is NaN).
  *   lse  optional fp32 [rows, h_q], contiguous (natural logarithm); dash_attn_key_mass_paged continues from it.
  *   workspace  dash_attn_paged_workspace_bytes(p) bytes, 256-byte aligned; it opens with a status word and arrival counters as
  *              the other workspaces do (dash_attn_reset_status once before the first use; dash_attn_last_status).  Calls that may
@@ -369,6 +371,8 @@ int dash_attn_attend_chunk_paged(const dash_paged_params* p, const void* Q, cons
  *   lse       fp32 [rows, h_q] as dash_attn_attend_chunk_paged writes it for the same Q and pages.
  *   mass_in, mass_out  fp32 [batch, h_kv, max_pages * page_size], contiguous; mass_in may be NULL (zeros) or mass_out itself.
  *             Slots of new tokens start from 0 whatever mass_in holds there; slots behind kv_len are left as they are.
+ *   Rows with lse -inf give no weight; queries are taken to be finite (a NaN in one reaches every slot that the row sees, and may
+ *   reach others of its tile).
  *   decay     finite; 1 accumulates.
  * No atomics: every sum has one owner and one order.  Workspace as above (its status word is used). */
 int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const void* Kpool, const int32_t* page_table,

@@ -230,17 +230,18 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
   copies_landed<0>();
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
+    if (l[i] != l[i]) m[i] = l[i];            // (a maximum passes over NaN; the row is not to be taken for one without keys)
     const long long rho = first + ty * RPT + i;
     if (rho >= n_rows) continue;
     const int tok = (int)(rho / pd.g_q), hh = (int)(rho - (long long)tok * pd.g_q);
     const long long row = s.q0 + tok, head = r * pd.g_q + hh;
     if (a.splits == 1) {
-      const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
 #pragma unroll
       for (int c = 0; c < CPT; ++c)
         *reinterpret_cast<float4*>(a.O + row * pd.os[0] + head * pd.os[1] + c * 64 + tx * 4) =
             make_float4(o[i][c].x * inv, o[i][c].y * inv, o[i][c].z * inv, o[i][c].w * inv);
-      if (tx == 0 && a.lse) a.lse[row * pd.h_q + head] = l[i] > 0.f ? (m[i] + __log2f(l[i])) * LN2 : -INFINITY;
+      if (tx == 0 && a.lse) a.lse[row * pd.h_q + head] = l[i] == 0.f ? -INFINITY : (m[i] + __log2f(l[i])) * LN2;
     } else {
       float* part = a.partials + (((long long)sp * pd.rows + row) * pd.h_q + head) * (D + 4);
 #pragma unroll
@@ -276,10 +277,10 @@ __global__ void __launch_bounds__(THREADS) chunk_merge_kernel(const __grid_const
 #pragma unroll
     for (int c = 0; c < VPL; ++c) o[c] = fmaf(part[k * step + c * 32 + lane], w, o[c]);
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int c = 0; c < VPL; ++c) a.O[row * pd.os[0] + head * pd.os[1] + c * 32 + lane] = o[c] * inv;
-  if (lane == 0 && a.lse) a.lse[unit] = l > 0.f ? (mx + __log2f(l)) * LN2 : -INFINITY;
+  if (lane == 0 && a.lse) a.lse[unit] = l == 0.f ? -INFINITY : (mx + __log2f(l)) * LN2;
 }
 
 // Attention weights per slot: a block keeps a K tile and walks the rows that see it.

@@ -46,6 +46,7 @@ constexpr int THREADS = 384;
 constexpr int REGS_SOFTMAX = 208, REGS_SERVICE = 88;
 static_assert(256 * REGS_SOFTMAX + 128 * REGS_SERVICE <= THREADS * 168, "what the block was launched with");
 constexpr uint32_t TMEM_COLS = 512;          // S0 [0,128), S1 [128,256), O0 [256,256+d), O1 behind it
+constexpr int OFF_ROW = 0x3fffffff;          // slots that a row sees which is not there: more than any cache has
 constexpr float RESCALE_LOG2 = 8.f;          // the running maximum moves only when it grew by more than this
 constexpr int MAX_SLOTS = 4096;              // unit slots (see the plan) of one launch
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -55,7 +56,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 __host__ __device__ constexpr bool on_fma(int pair) { return pair % 4 == 3; }
 
 enum Bar { Q_FULL = 0, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + KST, V_FULL = K_EMPTY + KST, V_EMPTY = V_FULL + VST, S_FULL = V_EMPTY + VST,
-           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 4, O_FREE = PV_DONE + 2, MEET = O_FREE + 2, E_DONE, N_BARS = E_DONE + 8 };      // P: [stage][part]; E: [stage][warp]
+           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 4, O_FREE = PV_DONE + 2, MEET = O_FREE + 2, E_DONE, DRAIN = E_DONE + 8, N_BARS = DRAIN + 2 };      // P: [stage][part]; E: [stage][warp]
 
 struct Misc {
   unsigned long long bar[N_BARS];
@@ -174,15 +175,22 @@ struct Cut {
   int row0, tokens, r, two, pad[3];
 };
 
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __log2f(l)) * LN2 : -INFINITY; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2; }      // (NaN stays NaN)
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : 1.f / l; }
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// Maxima that pass a NaN on, as the sums do: a row with one among its scores is NaN, not a row without keys.
+__device__ __forceinline__ float max2(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 
@@ -322,8 +330,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           }
         }
       }
-      // a wait ran out: let the copies already issued land (bounded) before the block retires
-      if (!ok && lane == 0) {
+      // Where a wait has run out, here or in another warp, the copies already issued land (bounded) before the block retires.
+      if (lane == 0) {
         for (int c = max(0, cnt - ST); c < cnt; ++c)
           for (int k = 0; k < 200000 && !ptx::mbar_try_wait(bar(full + c % ST), (c / ST) & 1); ++k) {}
         if (is_k && q_cnt > 0)
@@ -406,6 +414,10 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         it += steps;
         ++q_cnt;
       }
+      // what has been issued is let run out (bounded) before tensor memory goes back, whoever gave up
+      if (lead) ptx::mma_commit(bar(DRAIN + s));
+      for (int k = 0; k < 200000 && !ptx::mbar_try_wait(bar(DRAIN + s), 0); ++k) {}
+      __syncwarp();
     }
   } else {
     // =========================== softmax, epilogue ===========================
@@ -438,7 +450,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
       // Slots that the row sees, from the piece's first tile of this stage on (rows that are not there never ask for a mask), the
       // fewest of the warp, and the slots that hold anything.
       const int kv0 = (p.k0 + (two ? 0 : s)) * NT, stride = two ? NT : 2 * NT;
-      int seen = (!row_on ? 0x3fffffff : (int)min(max((long long)p.s.kv - p.s.q_len + p.t * TT + first + mt + 1, 0LL), (long long)p.s.valid)) - kv0;
+      int seen = (!row_on ? OFF_ROW : (int)min(max((long long)p.s.kv - p.s.q_len + p.t * TT + first + mt + 1, 0LL), (long long)p.s.valid)) - kv0;
       int fewest = __reduce_min_sync(0xffffffffu, seen), held = p.s.valid - kv0, c = base + (two ? 0 : s);
       // The two warps of a scheduler share its exponential unit.  Left alone they fall into step, both at their exponentials, then both
       // waiting for products: so they take turns.
@@ -490,13 +502,15 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
 #pragma unroll
             for (int k = 0; k < 8; ++k) ch[k] = max3(ch[k], __uint_as_float(sr[q + k]), __uint_as_float(sr[q + k + 8]));
 #pragma unroll
-          for (int k = 0; k < 8; ++k) ch[k] = fmaxf(ch[k], __uint_as_float(sr[NT - 8 + k]));
-          const float top = fmaxf(max3(ch[0], ch[1], ch[2]), fmaxf(max3(ch[3], ch[4], ch[5]), fmaxf(ch[6], ch[7]))) * c1;
+          for (int k = 0; k < 8; ++k) ch[k] = max2(ch[k], __uint_as_float(sr[NT - 8 + k]));
+          const float top = max3(max3(ch[0], ch[1], ch[2]), max3(ch[3], ch[4], ch[5]), max2(ch[6], ch[7])) * c1;
           float corr = 1.f;
           bool moved = false;
-          if (top > m_used + RESCALE_LOG2 || (m_used == -INFINITY && top > -INFINITY)) {
-            corr = exp2f(m_used - top);                // 0 when nothing was accumulated yet
-            m_used = top;
+          // (a NaN among the scores moves it too, and stays; rows that are not there, whose `seen` is beyond any cache, never do)
+          if (!(top <= m_used + RESCALE_LOG2) && seen < OFF_ROW / 2) {
+            const float now = max2(m_used, top);
+            corr = exp2f(m_used - now);                // 0 when nothing was accumulated yet
+            m_used = now;
             moved = true;
           }
           l *= corr;
@@ -590,7 +604,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         __syncwarp();
       };
       if (whole && p.two) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = reciprocal(l);
 #pragma unroll 1
         for (int q = 0; q < HD / 32 && warp_on; ++q) {
           uint32_t o[32], w[16];
@@ -645,9 +659,9 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           if (s == 0 && warp_on) {
             float2 other = make_float2(-INFINITY, 0.f);
             if (row_on) other = __ldcg(reinterpret_cast<const float2*>(part + 128 * HD) + m);
-            const float top = fmaxf(m_used, other.x);
-            const float w0 = m_used > -INFINITY ? exp2f(m_used - top) : 0.f, w1 = other.x > -INFINITY ? exp2f(other.x - top) : 0.f;
-            const float sm = fmaf(l, w0, other.y * w1), inv = sm > 0.f ? 1.f / sm : 0.f;
+            const float top = max2(m_used, other.x);
+            const float w0 = m_used == -INFINITY ? 0.f : exp2f(m_used - top), w1 = other.x == -INFINITY ? 0.f : exp2f(other.x - top);
+            const float sm = fmaf(l, w0, other.y * w1), inv = reciprocal(sm);
 #pragma unroll 1
             for (int q = 0; q < HD / 32; ++q) {
               uint32_t o[32], w[16];
@@ -655,7 +669,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
                 x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (w1 > 0.f) x[k] = __ldcg(reinterpret_cast<const float4*>(part) + (q * 8 + k) * 128 + m);
+                if (other.x != -INFINITY) x[k] = __ldcg(reinterpret_cast<const float4*>(part) + (q * 8 + k) * 128 + m);
               }
               __syncwarp();
               DASH_TMEM_LD32(o, o_addr + q * 32);
@@ -718,8 +732,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
       float4 x[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[q] = __ldcg(reinterpret_cast<const float4*>(part) + (col / 4 + q) * 128 + m);
-      if (ml.x > -INFINITY) {                // (a part without a key has nothing in its place)
-        const float top = fmaxf(mx, ml.x), corr = exp2f(mx - top), w = exp2f(ml.x - top);
+      if (ml.x != -INFINITY) {               // (a part without a key has nothing in its place)
+        const float top = max2(mx, ml.x), corr = exp2f(mx - top), w = exp2f(ml.x - top);
         mx = top;
         sm = fmaf(ml.y, w, sm * corr);
 #pragma unroll
@@ -733,7 +747,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
   const long long row = (long long)c.row0 + token, head = (long long)c.r * pd.g_q + m % pd.g_q;
   if (P == 1) {
     if (!on) return;
-    const float inv = sm > 0.f ? 1.f / sm : 0.f;
+    const float inv = reciprocal(sm);
     __nv_bfloat16* op = a.O + row * pd.os[0] + head * pd.os[1] + col;
 #pragma unroll
     for (int q = 0; q < 8; q += 2)
@@ -754,7 +768,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
     const int r2 = e >> 4, q = (e & 15) * 2;
     if (r2 >= c.tokens * pd.g_q) continue;
     float top = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
-    for (int k = 0; k < P; ++k) top = fmaxf(top, buf[k * span + r2][32]);
+    for (int k = 0; k < P; ++k) top = max2(top, buf[k * span + r2][32]);
     for (int k = 0; k < P; ++k) {
       const float* b = buf[k * span + r2];
       if (b[32] == -INFINITY) continue;
@@ -763,7 +777,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
       x = fmaf(b[q], w, x);
       y = fmaf(b[q + 1], w, y);
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = reciprocal(l);
     const long long orow = (long long)c.row0 + r2 / pd.g_q, ohead = (long long)c.r * pd.g_q + r2 % pd.g_q;
     *reinterpret_cast<uint32_t*>(a.O + orow * pd.os[0] + ohead * pd.os[1] + col + q) = pack2(x * inv, y * inv);
     if (col == 0 && q == 0 && a.lse) a.lse[orow * pd.h_q + ohead] = lse_of(top, l);

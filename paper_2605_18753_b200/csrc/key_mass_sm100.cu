@@ -36,7 +36,7 @@ constexpr uint32_t TMEM_COLS = 512;          // [K tile][S buffer] of 128 column
 constexpr int MAX_SEQS = 2048;               // sequences of one launch
 constexpr float LOG2E = 1.4426950408889634f;
 
-enum Bar { Q_FULL = 0, Q_EMPTY = 2, L_FULL = 4, S_FULL = 6, S_EMPTY = 10, R_FULL = 14, R_EMPTY = 16, K_FULL = 18, K_EMPTY = 21, N_BARS = 24 };
+enum Bar { Q_FULL = 0, Q_EMPTY = 2, L_FULL = 4, S_FULL = 6, S_EMPTY = 10, R_FULL = 14, R_EMPTY = 16, K_FULL = 18, K_EMPTY = 21, DRAIN = 24, N_BARS };
 
 // Warpgroups of sums per K tile, and threads of a block.
 template <int NQ> constexpr int GROUPS = NQ == 128 ? 2 : 1;
@@ -312,7 +312,7 @@ key_mass_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
       }
     }
-    if (!ok && lane == 0) {        // let the copies already issued land (bounded) before the block retires
+    if (lane == 0) {               // where a wait has run out, here or in another warp, the copies already issued land (bounded) first
       for (int c = max(0, kc - LY::KB); c < kc; ++c)
         for (int k = 0; k < 200000 && !ptx::mbar_try_wait(bar(K_FULL + c % LY::KB), (c / LY::KB) & 1); ++k) {}
       for (int c = max(0, qc - 2); c < qc; ++c)
@@ -392,6 +392,10 @@ key_mass_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       }
       ++kc;
     }
+    // what has been issued is let run out (bounded) before tensor memory goes back, whoever gave up
+    if (lead) ptx::mma_commit(bar(DRAIN));
+    for (int k = 0; k < 200000 && !ptx::mbar_try_wait(bar(DRAIN), 0); ++k) {}
+    __syncwarp();
   } else if (warp < SUM_WARPS) {
     // =========================== sums ===========================
     const int grp = warp >> 2, s = grp / GROUPS<NQ>, part = grp % GROUPS<NQ>, m = tid & 127;      // K tile, columns' share, row = TMEM lane

@@ -273,6 +273,52 @@ def test_offsets_beyond_32_bits():
     assert (kept == want).all() and torch.equal(K[pages - 1, :20], kn[want]) and torch.equal(V[pages - 1, :20], vn[want])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kv", [[40, 300], [9000, 5000]])
+def test_a_nan_query_stays_in_its_row(dtype, kv):
+    """In whole units and in units cut among blocks."""
+    c = Cache([3, 40], kv, h_q=8, h_kv=2, d=128, page=64, dtype=dtype)
+    c.attend()
+    O, lse = c.O.clone(), c.lse.clone()
+    c.Q[1, 2, 5] = float("nan")
+    c.Q[20, 7, 100] = float("nan")
+    c.attend()
+    hit = torch.zeros(c.rows, 8, dtype=torch.bool, device=DEV)
+    hit[1, 2] = hit[20, 7] = True
+    assert torch.isnan(c.O[hit]).all() and torch.isnan(c.lse[hit]).all()
+    assert torch.equal(c.O[~hit], O[~hit]) and torch.equal(c.lse[~hit], lse[~hit])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("q,kv", [([3, 40], [40, 300]), ([3, 40], [9000, 5000]), ([1, 1], [9000, 64])])
+def test_a_nan_key_reaches_the_rows_that_see_it(q, kv, dtype):
+    c = Cache(q, kv, h_q=8, h_kv=2, d=128, page=64, dtype=dtype)
+    c.attend()
+    O, lse = c.O.clone(), c.lse.clone()
+    slot = kv[1] - (20 if q[1] > 20 else 1)                  # in sequence 1, head 1; its last 20 tokens (or the one) see it
+    c.Kpool[int(c.table[1, slot // 64]), slot % 64, 1, 7] = float("nan")
+    c.attend()
+    hit = torch.zeros(c.rows, 8, dtype=torch.bool, device=DEV)
+    hit[q[0] + q[1] - (kv[1] - slot): q[0] + q[1], 4:] = True
+    assert torch.isnan(c.O[hit]).all() and torch.isnan(c.lse[hit]).all()
+    assert torch.equal(c.O[~hit], O[~hit]) and torch.equal(c.lse[~hit], lse[~hit])
+
+
+def test_an_error_in_the_status_word_ends_the_call_and_stays():
+    """A workspace whose status word holds an error: the blocks give up at the first wait that is not over at once, everything they have
+    issued runs out, and the word keeps the first error until it is reset; then the workspace serves again."""
+    c = Cache([1, 300], [4000, 900], h_q=8, h_kv=2, d=128, page=64, dtype=BF)
+    mass = torch.zeros(2, 2, c.cap, device=DEV)
+    for _ in range(3):
+        c.ws[:4] = torch.tensor([0xf9, 0xff, 0xff, 0xff], dtype=torch.uint8)              # DASH_ERR_TIMEOUT
+        B.dash_attn_attend_chunk_paged(c.p, c.Q, c.Kpool, c.Vpool, c.table, c.q_start, c.kv_len, c.O, c.lse, c.ws)
+        B.dash_attn_key_mass_paged(c.p, c.Q, c.Kpool, c.table, c.q_start, c.kv_len, c.lse, None, mass, c.ws)
+        assert B.dash_attn_last_status(c.ws) == -7
+    B.dash_attn_reset_status(c.ws)
+    c.attend()
+    c.check_attention()
+
+
 # ---------------------------------------------------------------- rotary positions
 
 def rope_tolerance(x, ref, dtype, pairs, interleaved):
