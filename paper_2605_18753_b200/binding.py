@@ -443,6 +443,11 @@ def _refuse(where, dtype, ints, floats, tensors):
                                  f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
+def _sizes(where, **pairs):
+    bad = [f"{name} {got}, not {want}" for name, (got, want) in pairs.items() if got != want]
+    raise ValueError(f"{where}: sizes that do not fit the parameters: " + ", ".join(bad))
+
+
 # A short call is a kernel of a few microseconds, so what these checks cost counts: one expression on the way that is taken, the search
 # for the culprit only behind it.
 
@@ -452,13 +457,15 @@ def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
     dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
     if not (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()):
         _refuse("dash_attn_rope", dt, (positions,), (), ())
-    for x, y in ((Q, Qout), (K, Kout)):
+    for x, y, h in ((Q, Qout, p.h_q), (K, Kout, p.h_kv)):
         if x is None and y is None:
             continue
         if x is None or y is None:
             raise ValueError("dash_attn_rope: every input has an output")
         if not (x.dtype is dt and y.dtype is dt and x.get_device() == dev and y.get_device() == dev):
             _refuse("dash_attn_rope", dt, (), (), (x, y))
+        if x.shape != (p.batch, p.seq_q, h, p.head_dim) or x.shape != y.shape:
+            raise ValueError("dash_attn_rope: tensors are [batch, seq, heads, head_dim] of the parameters, an output like its input")
         if x is not y and not (x.is_contiguous() and y.is_contiguous()) and x.stride() != y.stride():
             raise ValueError("dash_attn_rope: an output has the strides of its input")
     if positions.numel() != rope.axes * p.batch * p.seq_q:
@@ -481,7 +488,17 @@ def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Q
             and (positions is None or (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()))
             and (Q is None or (Q.dtype is dt and Q.get_device() == dev)) and (Qout is None or (Qout.dtype is dt and Qout.get_device() == dev))):
         _refuse("dash_attn_append_paged", dt, (positions, q_start, kv_len, page_table), (), (Q, Qout, K, V, Kpool, Vpool))
-    if positions is not None and positions.numel() != rope.axes * p.rows:
+    n, rows = p.batch, p.rows
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
+            and Vpool.size(0) == p.num_pages and K.size(0) == rows and V.size(0) == rows and (Q is None or Q.size(0) == rows)
+            and (Qout is None or Qout.size(0) == rows)):
+        _sizes("dash_attn_append_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
+               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages),
+               K=(K.size(0), rows), V=(V.size(0), rows), Q=(rows if Q is None else Q.size(0), rows),
+               Qout=(rows if Qout is None else Qout.size(0), rows))
+    if (rope is None) != (positions is None):
+        raise ValueError("dash_attn_append_paged: rope and positions come together")
+    if positions is not None and positions.numel() != rope.axes * rows:
         raise ValueError("positions must be [axes, rows]")
     rc = (_lib or lib()).dash_attn_append_paged(
         ctypes.byref(p), None if rope is None else ctypes.byref(rope), None if positions is None else positions.data_ptr(),
@@ -515,6 +532,12 @@ def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len
             and Vpool.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
             and (lse is None or (lse.dtype is _F32 and lse.get_device() == dev and lse.is_contiguous()))):
         _refuse("dash_attn_attend_chunk_paged", dt, (page_table, q_start, kv_len), (lse,), (Q, Kpool, Vpool, O))
+    n, rows = p.batch, p.rows
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
+            and Vpool.size(0) == p.num_pages and Q.size(0) == rows and O.size(0) == rows and (lse is None or lse.numel() == rows * p.h_q)):
+        _sizes("dash_attn_attend_chunk_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
+               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages),
+               Q=(Q.size(0), rows), O=(O.size(0), rows), lse=(rows * p.h_q if lse is None else lse.numel(), rows * p.h_q))
     rc = (_lib or lib()).dash_attn_attend_chunk_paged(
         ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
         O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
@@ -533,6 +556,14 @@ def dash_attn_key_mass_paged(p, Q, Kpool, page_table, q_start, kv_len, lse, mass
             and lse.is_contiguous() and mass_out.is_contiguous()
             and (mass_in is None or (mass_in.dtype is _F32 and mass_in.get_device() == dev and mass_in.is_contiguous()))):
         _refuse("dash_attn_key_mass_paged", dt, (page_table, q_start, kv_len), (lse, mass_in, mass_out), (Q, Kpool))
+    n, slots = p.batch, p.batch * p.h_kv * p.max_pages * p.page_size
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
+            and Q.size(0) == p.rows and lse.numel() == p.rows * p.h_q and mass_out.numel() == slots
+            and (mass_in is None or mass_in.numel() == slots)):
+        _sizes("dash_attn_key_mass_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
+               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Q=(Q.size(0), p.rows),
+               lse=(lse.numel(), p.rows * p.h_q), mass_in=(slots if mass_in is None else mass_in.numel(), slots),
+               mass_out=(mass_out.numel(), slots))
     rc = (_lib or lib()).dash_attn_key_mass_paged(
         ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), lse.data_ptr(),
         decay, None if mass_in is None else mass_in.data_ptr(), mass_out.data_ptr(), workspace.data_ptr(), workspace.numel(),
@@ -554,13 +585,23 @@ def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_l
             and kept.is_contiguous() and new_len.is_contiguous() and dst_table.is_contiguous() and mass.is_contiguous()
             and (mass_out is None or (mass_out.dtype is _F32 and mass_out.get_device() == dev and mass_out.is_contiguous()))):
         _refuse("dash_attn_evict_paged", dt, (kv_len, page_table, kept, new_len, dst_table), (mass, mass_out), (Kpool, Vpool, Kdst, Vdst))
-    shape = Kdst.shape
+    n, groups, shape = p.batch, p.batch * p.h_kv, Kdst.shape
+    width = dst_table.size(-1)
+    if not (kv_len.numel() == n and new_len.numel() == n and page_table.numel() == n * p.max_pages and dst_table.numel() == n * width
+            and kept.numel() == groups * keep and mass.numel() == groups * p.max_pages * p.page_size
+            and (mass_out is None or mass_out.numel() == groups * width * p.page_size) and Kpool.size(0) == p.num_pages
+            and Vpool.size(0) == p.num_pages and Vdst.shape == shape):
+        slots, out = groups * p.max_pages * p.page_size, groups * width * p.page_size
+        _sizes("dash_attn_evict_paged", kv_len=(kv_len.numel(), n), new_len=(new_len.numel(), n),
+               page_table=(page_table.numel(), n * p.max_pages), dst_table=(dst_table.numel(), n * width), kept=(kept.numel(), groups * keep),
+               mass=(mass.numel(), slots), mass_out=(out if mass_out is None else mass_out.numel(), out),
+               Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages), Vdst=(tuple(Vdst.shape), tuple(shape)))
     if shape[1:] != Kpool.shape[1:] or not (Kdst.is_contiguous() and Kpool.is_contiguous() or Kdst.stride() == Kpool.stride()) \
             or not (Vdst.is_contiguous() and Vpool.is_contiguous() or Vdst.stride() == Vpool.stride()):
         raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' page size, heads and strides")
     rc = (_lib or lib()).dash_attn_evict_paged(
         ctypes.byref(p), keep, sinks, recent, mass.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(),
-        kept.data_ptr(), new_len.data_ptr(), dst_table.data_ptr(), dst_table.shape[1], shape[0], Kdst.data_ptr(), Vdst.data_ptr(),
+        kept.data_ptr(), new_len.data_ptr(), dst_table.data_ptr(), width, shape[0], Kdst.data_ptr(), Vdst.data_ptr(),
         None if mass_out is None else mass_out.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         raise DashError(rc, "dash_attn_evict_paged")

@@ -189,3 +189,49 @@ def test_binding_refuses_wrong_shapes_and_types():
         B.params_for_paged(pool, pool, table, h_q=4, Q=torch.zeros(5, 2, 64, dtype=torch.bfloat16))
     p = B.params_for_paged(pool, None, table, h_q=4, rows=0)
     assert (p.batch, p.rows, p.page_size, p.max_pages, p.num_pages) == (1, 0, 16, 2, 3)
+
+
+def test_binding_refuses_sizes_that_do_not_fit_the_parameters(monkeypatch):
+    """What a kernel would write or read past the end of is refused before the library is called (tensors of the CPU here, taken for
+    those of the current device)."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: pytest.fail("the call went through"), raising=False)
+    bf, i32 = torch.bfloat16, torch.int32
+    K, V = torch.zeros(5, 16, 2, 64, dtype=bf), torch.zeros(5, 16, 2, 64, dtype=bf)
+    table, q_start, kv_len = torch.zeros(3, 4, dtype=i32), torch.zeros(4, dtype=i32), torch.zeros(3, dtype=i32)
+    Q, kn, pos = torch.zeros(6, 4, 64, dtype=bf), torch.zeros(6, 2, 64, dtype=bf), torch.zeros(1, 6, dtype=i32)
+    lse, mass, ws = torch.zeros(6, 4), torch.zeros(3, 2, 64), torch.zeros(1, dtype=torch.uint8)
+    kept, new_len = torch.zeros(3, 2, 8, dtype=i32), torch.zeros(3, dtype=i32)
+    p = B.params_for_paged(K, V, table, h_q=4, Q=Q, O=Q)
+    rope = B.make_rope([1.0] * 32)
+    args = {
+        "append": dict(rope=rope, positions=pos, q_start=q_start, kv_len=kv_len, page_table=table, Q=Q, Qout=Q, K=kn, V=kn, Kpool=K, Vpool=V),
+        "attend_chunk": dict(Q=Q, Kpool=K, Vpool=V, page_table=table, q_start=q_start, kv_len=kv_len, O=Q, lse=lse, workspace=ws),
+        "key_mass": dict(Q=Q, Kpool=K, page_table=table, q_start=q_start, kv_len=kv_len, lse=lse, mass_in=mass, mass_out=mass, workspace=ws),
+        "evict": dict(mass=mass, kv_len=kv_len, page_table=table, Kpool=K, Vpool=V, kept=kept, new_len=new_len, dst_table=table, Kdst=K,
+                      Vdst=V, mass_out=mass, keep=8),
+    }
+    for name, kw in args.items():
+        call = getattr(B, f"dash_attn_{name}_paged")
+        for arg, t in kw.items():
+            if arg in ("rope", "workspace", "keep") or (name == "evict" and arg in ("Kdst", "dst_table")):
+                continue
+            short = t[..., :-1].contiguous() if t.dim() == 1 else t[:-1].contiguous()
+            if arg == "positions":
+                short = t[:, :-1].contiguous()
+            with pytest.raises(ValueError):
+                call(p, **{**kw, arg: short})
+    with pytest.raises(ValueError):
+        B.dash_attn_append_paged(p, **{**args["append"], "rope": None})
+    with pytest.raises(ValueError):
+        B.dash_attn_append_paged(p, **{**args["append"], "positions": None})
+    with pytest.raises(ValueError):
+        B.dash_attn_evict_paged(p, **{**args["evict"], "dst_table": table[:2].contiguous()})
+    with pytest.raises(ValueError):
+        B.dash_attn_evict_paged(p, **{**args["evict"], "Kdst": K[:4].contiguous()})
+    x = torch.zeros(2, 8, 4, 64, dtype=bf)
+    rp = B.params_for_prefill(x, x[:, :, :2].contiguous(), x[:, :, :2].contiguous(), x, block=16, alpha=1.5)
+    pos = torch.zeros(1, 2, 8, dtype=i32)
+    for a, b in ((x, x[:, :7].contiguous()), (x[:1].contiguous(), x[:1].contiguous()), (x[:, :7].contiguous(), x[:, :7].contiguous())):
+        with pytest.raises(ValueError):
+            B.dash_attn_rope(rp, rope, pos, a, None, b, None)
