@@ -273,6 +273,78 @@ def test_offsets_beyond_32_bits():
     assert (kept == want).all() and torch.equal(K[pages - 1, :20], kn[want]) and torch.equal(V[pages - 1, :20], vn[want])
 
 
+def test_one_sequence_over_several_launches():
+    """A sequence with more units than one launch's plan holds (two tokens a unit), behind another one."""
+    c = Cache([200, 8300, 1], [200, 60, 33], h_q=128, h_kv=1, d=64, page=16, dtype=BF, q_scale=1.0)
+    c.attend()
+    c.check_attention()
+    out = torch.full((3, 1, c.cap), 9.0, device=DEV)
+    B.dash_attn_key_mass_paged(c.p, c.Q, c.Kpool, c.table, c.q_start, c.kv_len, c.lse, None, out, c.ws)
+    assert B.dash_attn_last_status(c.ws) == 0
+    c.check_mass(None, 1.0, out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("q_lens,kv_lens,h_q,h_kv", [
+    ([1] * 39 + [100], [50 + k for k in range(39)] + [3000], 4, 2),      # few rows a sequence on average, one with many
+    ([300], [3001], 4, 1), ([1, 200], [2500, 900], 8, 2), ([40], [9000], 2, 1)])
+def test_weights_of_long_caches_are_divided_among_blocks(q_lens, kv_lens, h_q, h_kv, dtype):
+    c = Cache(q_lens, kv_lens, h_q=h_q, h_kv=h_kv, d=64, page=32, dtype=dtype, seed=6)
+    c.attend()
+    mass = torch.rand(len(q_lens), h_kv, c.cap, device=DEV)
+    out = torch.full_like(mass, 9.0)
+    for _ in range(2):
+        B.dash_attn_key_mass_paged(c.p, c.Q, c.Kpool, c.table, c.q_start, c.kv_len, c.lse, mass, out, c.ws, decay=0.75)
+        assert B.dash_attn_last_status(c.ws) == 0
+        c.check_mass(mass, 0.75, out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rising", [True, False])
+def test_running_maximum_that_moves_with_every_tile(rising, dtype):
+    """Scores that climb, or fall, by several powers of two from each tile of keys to the next."""
+    c = Cache([1, 300, 7], [3000, 1500, 900], h_q=8, h_kv=2, d=128, page=64, dtype=dtype)
+    u = torch.randn(128, generator=torch.Generator().manual_seed(8))
+    c.Q.copy_((u * torch.linspace(0.5, 2.0, 8)[:, None]).to(dtype).to(DEV).expand_as(c.Q))
+    for b, n in enumerate(c.kv_lens):
+        t = torch.linspace(0, 1, n) if rising else torch.linspace(1, 0, n)
+        c.Kc[b] = (u * (4 * t)[:, None, None] + 0.1 * c.Kc[b].float()).to(dtype)
+        for k in range(-(-n // 64)):
+            part = c.Kc[b][k * 64:k * 64 + 64]
+            c.Kpool[c.table[b, k].long(), :len(part)] = part.to(DEV)
+    c.attend()
+    c.check_attention()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_weights_and_eviction_at_lengths_out_of_range(dtype):
+    """kv_len beyond the table counts as far as there are slots, a negative one as nothing; a page that is none reads as zeros."""
+    c = Cache([2, 2], [64, 64], h_q=4, h_kv=2, d=64, page=32, dtype=dtype)
+    c.table[0, 1] = 1 << 29
+    c.Kc[0][32:] = 0
+    c.kv_len.copy_(torch.tensor([1000, -5]))
+    c.attend()
+    mass = torch.rand(2, 2, 64, device=DEV)
+    out = torch.full_like(mass, 9.0)
+    B.dash_attn_key_mass_paged(c.p, c.Q, c.Kpool, c.table, c.q_start, c.kv_len, c.lse, mass, out, c.ws, decay=0.5)
+    s = np.einsum("ihd,thd->iht", np64(c.Q[:2]), np64(c.Kc[0]).repeat(2, axis=1)) / 8
+    want = 0.5 * np64(mass[0]) + np.exp(s - np64(c.lse[:2])[..., None]).sum(0).reshape(2, 2, 64).sum(1)
+    es = c.score_noise(0, np64(c.Q[:2]))
+    assert (np.abs(np64(out[0]) - want) <= (es + 2.0 ** -20 * (1 + np.abs(np64(c.lse[:2])).max()) + 2.0 ** -19) * want).all()
+    assert (out[1] == 9).all()
+    for keep in (40, 64, 70):
+        kept, new_len, table, K, V, moved = _evict(c, mass, keep, 2, 5, True)
+        assert new_len == [min(64, keep), 0] and (kept[1] == -1).all()
+        for r in range(2):
+            want = po.evicted(np64(mass[0, r]), 64, keep, 2, 5)
+            assert kept[0, r, :len(want)].tolist() == want.tolist() and (kept[0, r, len(want):] == -1).all()
+            assert torch.equal(moved[0, r, :len(want)], mass[0, r].cpu()[torch.from_numpy(want)])
+            first = torch.from_numpy(want[:32])                      # the rows of the one page that there is
+            src = c.Kpool[c.table[0, 0].long(), :, r].cpu()
+            old = torch.where((first < 32)[:, None], src[first.clamp(max=31)].float(), torch.zeros(1))
+            assert torch.equal(K[table[0, 0].long(), :len(first), r].float(), old)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("kv", [[40, 300], [9000, 5000]])
 def test_a_nan_query_stays_in_its_row(dtype, kv):
