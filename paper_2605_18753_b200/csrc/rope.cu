@@ -8,10 +8,11 @@
 //
 // Memory-bound: every element is read and written once.  A thread owns one piece of the head (N pairs: two 16-byte vectors) of one
 // token, forms its cosines and sines in registers and takes the piece through its share of the heads, four heads on their way
-// at once; the eight lanes of a head cover whole lines.  8192 tokens, 40 heads, d 128: 32.0 us (5.2 TB/s, 80 % of the measured copy);
-// with a table in shared memory for all heads of a token 42 (bank conflicts, a barrier), one head on its way at a time 45.  12,300
-// tokens with their K and V into pages: 44 us (4.7 TB/s).  Three blocks per SM for the rotation alone, two where the pages' addresses
-// take registers as well.
+// at once; the eight lanes of a head cover whole lines.  8192 tokens, 40 heads, d 128: 29.8 us (5.6 TB/s, 86 % of the measured copy);
+// with a table in shared memory for all heads of a token 42 (bank conflicts, a barrier), one head on its way at a time 45, eight 34,
+// four with the next four behind them 35 to 44.  12,300 tokens with their K and V into pages: 39.3 us (5.3 TB/s).
+// Small blocks: each goes through phases (loads, cosines, stores), and the more of them share an SM the better the phases mix; of 64, 128
+// and 256 threads at the same number of threads per SM 29.8 / 30.7 / 32.3 us, and 39.3 / 39.8 / 44.6 into pages.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -20,7 +21,8 @@ namespace dash {
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 64;
+constexpr int ROPE_TOKENS = 2, APPEND_TOKENS = 4;      // per block, at most (4 and 2: 32.7 us alone, 40.8 into pages)
 
 __device__ __forceinline__ float2 cos_sin_of_turns(unsigned long long freq, int pos) {
   const unsigned long long turns = freq * (unsigned long long)(long long)pos;
@@ -197,7 +199,7 @@ struct RopeArgs {
 };
 
 template <typename T, bool SCALAR, bool IL>
-__global__ void __launch_bounds__(THREADS, 3) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(THREADS, 10) rope_kernel(const __grid_constant__ RopeArgs a) {
   using P = Piece<T, SCALAR, IL>;
   const Share sh(a.d / (2 * P::N), a.tokens);
   chain_wait();
@@ -225,10 +227,9 @@ struct AppendArgs {
   int tokens;     // per block
 };
 
-constexpr int APPEND_TOKENS = 8;
 
 template <typename T, bool SCALAR, bool IL>
-__global__ void __launch_bounds__(THREADS, 2) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(THREADS, 8) append_kernel(const __grid_constant__ AppendArgs a) {
   using P = Piece<T, SCALAR, IL>;
   __shared__ long long page_of[APPEND_TOKENS];    // physical page, -1: no slot, -2: not a row of any sequence
   __shared__ int tok_of[APPEND_TOKENS];
@@ -286,11 +287,11 @@ bool by_vectors(const RopeTable& rt, int d, int n) {
   return rt.pairs % n == 0 && (d - 2 * rt.pairs) % (2 * n) == 0;
 }
 
-// Tokens per block: as few as leave the machine blocks to fill it (a token's heads are then shared by more threads), eight where there
-// are many (the cosines of a piece serve more heads).
-int tokens_per_block(long long tokens, int pieces) {
-  int t = tokens >= 8LL * 4 * current_sm_count() ? 8 : tokens >= 4LL * current_sm_count() ? 2 : 1;
-  while (t * pieces > THREADS) t >>= 1;
+// Tokens per block: `most` where there are many (the cosines of a piece serve more heads), fewer where that would leave the machine
+// short of blocks (eight per SM; a token's heads are then shared by more threads).
+int tokens_per_block(long long tokens, int pieces, int most) {
+  int t = most;
+  while (t > 1 && (t * pieces > THREADS || tokens < 8LL * t * current_sm_count())) t >>= 1;
   return t;
 }
 
@@ -298,7 +299,7 @@ template <typename T>
 cudaError_t launch_rope_t(RopeArgs& a, cudaStream_t st) {
   const long long total = (long long)a.batch * a.n;
   const bool vec = by_vectors(a.rt, a.d, Vec<T>::N);
-  a.tokens = tokens_per_block(total, a.d / (vec ? 2 * Vec<T>::N : 2));
+  a.tokens = tokens_per_block(total, a.d / (vec ? 2 * Vec<T>::N : 2), ROPE_TOKENS);
   const unsigned blocks = (unsigned)((total + a.tokens - 1) / a.tokens);
   auto kern = vec ? (a.rt.interleaved ? rope_kernel<T, false, true> : rope_kernel<T, false, false>)
                   : (a.rt.interleaved ? rope_kernel<T, true, true> : rope_kernel<T, true, false>);
@@ -310,7 +311,7 @@ cudaError_t launch_rope_t(RopeArgs& a, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_append_t(AppendArgs& a, cudaStream_t st) {
   const bool vec = by_vectors(a.rt, a.pd.d, Vec<T>::N);
-  a.tokens = tokens_per_block(a.pd.rows, a.pd.d / (vec ? 2 * Vec<T>::N : 2));
+  a.tokens = tokens_per_block(a.pd.rows, a.pd.d / (vec ? 2 * Vec<T>::N : 2), APPEND_TOKENS);
   const unsigned blocks = (unsigned)((a.pd.rows + a.tokens - 1) / a.tokens);
   auto kern = vec ? (a.rt.interleaved ? append_kernel<T, false, true> : append_kernel<T, false, false>)
                   : (a.rt.interleaved ? append_kernel<T, true, true> : append_kernel<T, true, false>);
