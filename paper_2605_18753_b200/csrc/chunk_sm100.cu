@@ -702,32 +702,34 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
   if (tid == 0 && misc->abort_flag) report_error(a.sb, DASH_ERR_TIMEOUT, 301);
 }
 
-// Joins the partial results of a cut unit: block (x, y) the unit that attention block x cuts at its end, 32 columns.  Threads share a
-// row where there are few: P of them take every P-th part each and meet in shared memory.
-constexpr int JOIN_THREADS = 256;
+// Joins the partial results of a cut unit: block (x, y) the unit that attention block x cuts at its end, its y-th share.
+//   a unit of two row tiles (in few parts): 32 columns of all rows, a row per thread;
+//   fewer rows (in up to 2 x 148 parts, where one long cache is all there is): a share of the rows, a thread four columns of one,
+//   neighbouring threads neighbouring rows (as the parts lie), and what is left of the threads as P groups that take every P-th part and
+//   meet in shared memory, so that a hundred parts are no chain of a hundred loads (16 tokens over 27,000 slots: 34 us in all, 73
+//   with this case done as the other; shares by 32, or blocks of 512 threads, 28 to 31, but up to 4 us more where the parts are few).
+constexpr int JOIN_THREADS = 256, JOIN_SHARES = 16;
 template <int HD>
 __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_constant__ ChunkArgs a) {
-  __shared__ float buf[JOIN_THREADS][35];
+  constexpr int C4 = HD / 4;                          // pieces of four columns
+  __shared__ float4 out[JOIN_THREADS];                // [P][row][piece]
+  __shared__ float2 stat[JOIN_THREADS];               // [P][row]
+  static_assert(128 / JOIN_SHARES * C4 <= JOIN_THREADS, "a share is no more than a piece per thread");
   const PagedDims& pd = a.pd;
   chain_wait();
-  const int first = blockIdx.x, col = blockIdx.y * 32, tid = threadIdx.x;
+  const int first = blockIdx.x, tid = threadIdx.x;
   const Cut c = a.cuts[first];
   if (c.blocks == 0) return;
-  const int per = c.two ? 1 : 2, parts = c.blocks * per;
-  int span = JOIN_THREADS;                   // rows that threads are dealt to
-  if (!c.two)
-    while (span / 2 >= c.tokens * pd.g_q) span >>= 1;
-  const int P = JOIN_THREADS / span, rho = tid & (span - 1);
-  const int stage = c.two ? rho >> 7 : 0, m = c.two ? rho & 127 : rho, token = (c.two ? stage * a.TQ : 0) + m / pd.g_q;
-  const bool on = m < a.TQ * pd.g_q && token < c.tokens;
-  float mx = -INFINITY, sm = 0.f;
-  float4 acc[8];
+  if (c.two) {
+    const int col = blockIdx.y * 32, stage = tid >> 7, m = tid & 127, token = stage * a.TQ + m / pd.g_q;
+    if (col >= HD || m >= a.TQ * pd.g_q || token >= c.tokens) return;
+    float mx = -INFINITY, sm = 0.f;
+    float4 acc[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (on) {
+    for (int k = 0; k < 8; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-    for (int k = tid / span; k < parts; k += P) {
-      const float* part = partial_at<HD>(a, first + k / per, k < per ? 1 : 0, c.two ? stage : k % per);
+    for (int k = 0; k < c.blocks; ++k) {
+      const float* part = partial_at<HD>(a, first + k, k == 0 ? 1 : 0, stage);
       const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + 128 * HD) + m);
       float4 x[8];
 #pragma unroll
@@ -743,10 +745,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
         }
       }
     }
-  }
-  const long long row = (long long)c.row0 + token, head = (long long)c.r * pd.g_q + m % pd.g_q;
-  if (P == 1) {
-    if (!on) return;
+    const long long row = (long long)c.row0 + token, head = (long long)c.r * pd.g_q + m % pd.g_q;
     const float inv = reciprocal(sm);
     __nv_bfloat16* op = a.O + row * pd.os[0] + head * pd.os[1] + col;
 #pragma unroll
@@ -756,31 +755,55 @@ __global__ void __launch_bounds__(JOIN_THREADS) chunk_join_kernel(const __grid_c
     if (col == 0 && a.lse) a.lse[row * pd.h_q + head] = lse_of(mx, sm);
     return;
   }
-  buf[tid][32] = mx;
-  buf[tid][33] = sm;
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    buf[tid][4 * q] = acc[q].x; buf[tid][4 * q + 1] = acc[q].y; buf[tid][4 * q + 2] = acc[q].z; buf[tid][4 * q + 3] = acc[q].w;
+  const int rows = c.tokens * pd.g_q;
+  int span = 128;                             // the rows, up to a power of two; R of them are a share
+  while (span > 1 && span / 2 >= rows) span >>= 1;
+  const int R = max(1, span / JOIN_SHARES), row0 = blockIdx.y * R;
+  if (row0 >= rows) return;
+  const int parts = 2 * c.blocks, work = R * C4, P = JOIN_THREADS / work;
+  {
+    const int mine = tid / work, w = tid - mine * work, r = w & (R - 1), piece = w / R, m = row0 + r;
+    float mx = -INFINITY, sm = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m < rows) {
+#pragma unroll 8
+      for (int k = mine; k < parts; k += P) {
+        const float* part = partial_at<HD>(a, first + (k >> 1), k < 2 ? 1 : 0, k & 1);
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + 128 * HD) + m);
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(part) + piece * 128 + m);
+        if (ml.x != -INFINITY) {
+          const float top = max2(mx, ml.x), corr = exp2f(mx - top), wt = exp2f(ml.x - top);
+          mx = top;
+          sm = fmaf(ml.y, wt, sm * corr);
+          acc.x = fmaf(x.x, wt, acc.x * corr); acc.y = fmaf(x.y, wt, acc.y * corr);
+          acc.z = fmaf(x.z, wt, acc.z * corr); acc.w = fmaf(x.w, wt, acc.w * corr);
+        }
+      }
+    }
+    out[(mine * R + r) * C4 + piece] = acc;
+    if (piece == 0) stat[mine * R + r] = make_float2(mx, sm);
   }
   __syncthreads();
-  // a thread per row and pair of columns
-  for (int e = tid; e < span * 16; e += JOIN_THREADS) {
-    const int r2 = e >> 4, q = (e & 15) * 2;
-    if (r2 >= c.tokens * pd.g_q) continue;
-    float top = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
-    for (int k = 0; k < P; ++k) top = max2(top, buf[k * span + r2][32]);
+  for (int e = tid; e < R * (HD / 8); e += JOIN_THREADS) {
+    const int r = e / (HD / 8), q = e - r * (HD / 8), m = row0 + r;
+    if (m >= rows) continue;
+    float top = -INFINITY, l = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+    for (int k = 0; k < P; ++k) top = max2(top, stat[k * R + r].x);
     for (int k = 0; k < P; ++k) {
-      const float* b = buf[k * span + r2];
-      if (b[32] == -INFINITY) continue;
-      const float w = exp2f(b[32] - top);
-      l = fmaf(b[33], w, l);
-      x = fmaf(b[q], w, x);
-      y = fmaf(b[q + 1], w, y);
+      const float2 ml = stat[k * R + r];
+      if (ml.x == -INFINITY) continue;
+      const float wt = exp2f(ml.x - top);
+      const float4 u = out[(k * R + r) * C4 + 2 * q], v = out[(k * R + r) * C4 + 2 * q + 1];
+      l = fmaf(ml.y, wt, l);
+      x.x = fmaf(u.x, wt, x.x); x.y = fmaf(u.y, wt, x.y); x.z = fmaf(u.z, wt, x.z); x.w = fmaf(u.w, wt, x.w);
+      y.x = fmaf(v.x, wt, y.x); y.y = fmaf(v.y, wt, y.y); y.z = fmaf(v.z, wt, y.z); y.w = fmaf(v.w, wt, y.w);
     }
     const float inv = reciprocal(l);
-    const long long orow = (long long)c.row0 + r2 / pd.g_q, ohead = (long long)c.r * pd.g_q + r2 % pd.g_q;
-    *reinterpret_cast<uint32_t*>(a.O + orow * pd.os[0] + ohead * pd.os[1] + col + q) = pack2(x * inv, y * inv);
-    if (col == 0 && q == 0 && a.lse) a.lse[orow * pd.h_q + ohead] = lse_of(top, l);
+    const long long row = (long long)c.row0 + m / pd.g_q, head = (long long)c.r * pd.g_q + m % pd.g_q;
+    *reinterpret_cast<uint4*>(a.O + row * pd.os[0] + head * pd.os[1] + q * 8) =
+        make_uint4(pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv), pack2(y.x * inv, y.y * inv), pack2(y.z * inv, y.w * inv));
+    if (q == 0 && a.lse) a.lse[row * pd.h_q + head] = lse_of(top, l);
   }
 }
 
@@ -803,10 +826,14 @@ cudaError_t launch_hd(ChunkArgs& a, const CUtensorMap& tq, const CUtensorMap& tk
   for (long long s0 = 0; s0 < slots; s0 += MAX_SLOTS) {
     a.slot0 = (int)s0;
     a.n_slots = (int)(slots - s0 < MAX_SLOTS ? slots - s0 : MAX_SLOTS);
-    cudaError_t e = launch_chained(kern, dim3((unsigned)a.n_blocks), dim3(THREADS), Layout<HD>::smem(a.n_slots), st, tq, tk, tv, a);
+    // (the kernel uses a block per two tiles at most, and the tables bound their number)
+    const long long most = (long long)a.n_slots * ((a.pd.cap + NT - 1) / NT) * a.pd.h_kv;
+    const unsigned blocks = (unsigned)(most < 2LL * a.n_blocks ? (most + 1) / 2 : a.n_blocks);
+    cudaError_t e = launch_chained(kern, dim3(blocks), dim3(THREADS), Layout<HD>::smem(a.n_slots), st, tq, tk, tv, a);
     count_launch();
     if (e != cudaSuccess) return e;
-    e = launch_chained(chunk_join_kernel<HD>, dim3((unsigned)a.n_blocks, HD / 32), dim3(JOIN_THREADS), 0, st, a);
+    if (a.pd.cap <= NT) continue;              // units of one tile are not cut
+    e = launch_chained(chunk_join_kernel<HD>, dim3(blocks, JOIN_SHARES), dim3(JOIN_THREADS), 0, st, a);
     count_launch();
     if (e != cudaSuccess) return e;
   }
