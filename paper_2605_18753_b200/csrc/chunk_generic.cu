@@ -158,6 +158,9 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
     for (int c = 0; c < CPT; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   const float c1 = pd.sm_scale * LOG2E;
+  // A warp without a row only moves tiles (every warp reads the whole of K and V from shared memory: with one row of sixteen that was
+  // what took the time).
+  const bool busy = first + (ty & ~1) * RPT < n_rows;
   // K of a tile lands while the product with V of the tile before is formed, V while the scores are
   auto load_k = [&](int j) { load_tile<D, D + 4>(pd, a.K, pd.ks, r, ks, j & 1, ks); };
   auto load_v = [&](int j) { load_tile<D, D>(pd, a.V, pd.vs, r, ks, j & 1, vs); };
@@ -172,12 +175,12 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
     __syncthreads();
     const Where next(pd, table, tid < KT ? (j + 2) * KT + tid : s.valid, s.valid);
     float acc[RPT][4];
-    score_tile<D, RPT>(qs, ks, ty, tx, acc);
+    if (busy) score_tile<D, RPT>(qs, ks, ty, tx, acc);
     if (tid < KT) *where<D>(ks, tid, j & 1) = next.get(pd);
     __syncthreads();                                   // K has been read
     if (j + 1 < t1) load_k(j + 1); else copies_issued();
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) {
+    for (int i = 0; i < RPT && busy; ++i) {
       float mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(THREADS, 2) attend_chunk_generic_kernel(const 
     copies_landed<1>();                                // V
     __syncthreads();
 #pragma unroll 2
-    for (int k = 0; k < KT; k += 4) {
+    for (int k = 0; k < KT && busy; k += 4) {
       float4 p[RPT];
 #pragma unroll
       for (int i = 0; i < RPT; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (ty * RPT + i) * LDP + k);
@@ -315,10 +318,11 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
       if (first + ROWS < n_rows) load_rows<D, ROWS>(pd, a.Q, s, r, first + ROWS, q2 + (buf ^ 1) * ROWS * D); else copies_issued();
       copies_landed<1>();
       __syncthreads();
+      const bool busy = first + (ty & ~1) * RPT < n_rows;      // (by warps)
       float acc[RPT][4];
-      score_tile<D, RPT>(qs, ks, ty, tx, acc);
+      if (busy) score_tile<D, RPT>(qs, ks, ty, tx, acc);
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) {
+      for (int i = 0; i < RPT && busy; ++i) {
         const long long rho = first + ty * RPT + i;
         const int sees = row_sees(pd, s, rho);
         if (sees <= 0) continue;
@@ -326,7 +330,7 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
         const float lse = __ldg(a.lse_in + (long long)(s.q0 + tok) * pd.h_q + r * pd.g_q + hh) * LOG2E;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (j * KT + tx + 16 * k < sees) sum[k] += exp2f(fmaf(acc[i][k], c1, -lse));
+          if (j * KT + tx + 16 * k < sees && lse > -INFINITY) sum[k] += exp2f(fmaf(acc[i][k], c1, -lse));
       }
       __syncthreads();                                 // the rows have been read
     }

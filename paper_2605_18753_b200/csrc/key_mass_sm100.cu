@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(PAIR) mass_join_kernel(const __grid_constant__
   const MassCut c = a.cuts[first];
   if (c.blocks == 0) return;
   float total = a.parts[((long long)first * 2 + 1) * PAIR + threadIdx.x];
-#pragma unroll 4
+#pragma unroll 16
   for (int k = 1; k < c.blocks; ++k) total += a.parts[(long long)(first + k) * 2 * PAIR + threadIdx.x];
   const Seq s = load_seq(a.pd, a.q_start, a.kv_len, c.b);
   const int slot = c.slot0 + threadIdx.x;

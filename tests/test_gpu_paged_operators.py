@@ -300,6 +300,19 @@ def test_weights_of_long_caches_are_divided_among_blocks(q_lens, kv_lens, h_q, h
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_of_minus_infinity_give_no_weight(dtype):
+    """Whatever their scores are: a log-sum-exp of -inf says that the row has no weight to give."""
+    c = Cache([40, 1, 3], [200, 77, 300], h_q=8, h_kv=2, d=64, page=32, dtype=dtype)
+    c.attend()
+    given = c.lse.clone()
+    given[2], given[30, 5], given[40] = -torch.inf, -torch.inf, -torch.inf
+    out = torch.full((3, 2, c.cap), 9.0, device=DEV)
+    B.dash_attn_key_mass_paged(c.p, c.Q, c.Kpool, c.table, c.q_start, c.kv_len, given, None, out, c.ws)
+    c.lse.copy_(torch.where(torch.isneginf(given), torch.inf, given))      # to the formula: weights of exp(-inf)
+    c.check_mass(None, 1.0, out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rising", [True, False])
 def test_running_maximum_that_moves_with_every_tile(rising, dtype):
     """Scores that climb, or fall, by several powers of two from each tile of keys to the next."""
