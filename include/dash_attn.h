@@ -420,6 +420,11 @@ int64_t dash_attn_launch_count(void);
  *                      hanging or faulting anything. */
 void dash_attn_test_hooks(int64_t wait_limit_cycles, int32_t skip_own_k_load);
 
+/* The same kind of switch for the bf16 dash_attn_attend_chunk_paged: its loader holds back every other tile of values (the
+ * even ones, or with odd = 1 the odd ones) for `cycles` SM clocks (at most a million; 0 restores the default), as a busy
+ * memory would.  Results may not change. */
+void dash_attn_test_hold_loads(int64_t cycles, int32_t odd);
+
 const char* dash_attn_strerror(int status);
 
 #ifdef __cplusplus

@@ -33,6 +33,7 @@ EXPORTS = [
     "dash_attn_key_mass_paged", "dash_attn_evict_paged",
     "dash_attn_fwd_prefill", "dash_attn_fwd_decode", "dash_attn_reset_status", "dash_attn_last_status",
     "dash_attn_launch_count", "dash_attn_strerror", "dash_attn_test_hooks",
+    "dash_attn_test_hold_loads",
 ]
 
 
@@ -136,6 +137,8 @@ def lib() -> ctypes.CDLL:
         L.dash_attn_launch_count.argtypes = []
         L.dash_attn_test_hooks.restype = None
         L.dash_attn_test_hooks.argtypes = [c_int64, c_int32]
+        L.dash_attn_test_hold_loads.restype = None
+        L.dash_attn_test_hold_loads.argtypes = [c_int64, c_int32]
         L.dash_attn_strerror.restype = c_char_p
         L.dash_attn_strerror.argtypes = [ctypes.c_int]
         _lib = L
@@ -618,6 +621,11 @@ def dash_attn_last_status(workspace) -> int:
 def dash_attn_test_hooks(wait_limit_cycles: int = 0, skip_own_k_load: int = 0) -> None:
     """Test-suite switches (see the header); calling it without arguments restores the defaults."""
     lib().dash_attn_test_hooks(int(wait_limit_cycles), int(skip_own_k_load))
+
+
+def dash_attn_test_hold_loads(cycles: int = 0, odd: bool = False) -> None:
+    """Test-suite switch (see the header); calling it without arguments restores the default."""
+    lib().dash_attn_test_hold_loads(int(cycles), int(bool(odd)))
 
 
 def dash_attn_launch_count() -> int:

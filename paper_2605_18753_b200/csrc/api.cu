@@ -491,6 +491,12 @@ void dash_attn_test_hooks(int64_t wait_limit_cycles, int32_t skip_own_k_load) {
   h.skip_own_k_load = skip_own_k_load ? 1 : 0;
 }
 
+void dash_attn_test_hold_loads(int64_t cycles, int32_t odd) {
+  TestHooks& h = test_hooks();
+  h.hold_cycles = cycles <= 0 ? 0 : cycles < 1000000 ? cycles : 1000000;
+  h.hold_odd = odd ? 1 : 0;
+}
+
 const char* dash_attn_strerror(int status) {
   switch (status) {
     case DASH_OK: return "ok";

@@ -56,7 +56,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 __host__ __device__ constexpr bool on_fma(int pair) { return pair % 4 == 3; }
 
 enum Bar { Q_FULL = 0, Q_EMPTY, K_FULL, K_EMPTY = K_FULL + KST, V_FULL = K_EMPTY + KST, V_EMPTY = V_FULL + VST, S_FULL = V_EMPTY + VST,
-           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 4, O_FREE = PV_DONE + 2, MEET = O_FREE + 2, E_DONE, DRAIN = E_DONE + 8, N_BARS = DRAIN + 2 };      // P: [stage][part]; E: [stage][warp]
+           P_FULL = S_FULL + 2, PV_DONE = P_FULL + 4, O_FREE = PV_DONE + 2, MEET = O_FREE + 2, E_DONE, DRAIN = E_DONE + 8, V_SEEN = DRAIN + 2,
+           N_BARS };      // P: [stage][part]; E: [stage][warp]
 
 struct Misc {
   unsigned long long bar[N_BARS];
@@ -88,6 +89,8 @@ struct ChunkArgs {
   float* partials;
   struct Cut* cuts;
   StatusBlock* sb;
+  long long hold;                  // test hook: clocks that V tiles of one parity are held back (0: none)
+  int hold_odd;
 };
 
 // One block's share of a unit.
@@ -214,7 +217,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
   if (tid == 0) {
     misc->abort_flag = (sbase & 1023u) != 0u;
     for (int i = 0; i < N_BARS; ++i) ptx::mbar_init(bar(i), i >= P_FULL && i < PV_DONE ? 4 : i >= O_FREE && i < MEET ? 4 : i == MEET ? 8 :
-                                                        i == Q_EMPTY || (i >= K_EMPTY && i < V_FULL) || (i >= V_EMPTY && i < S_FULL) ? 2 : 1);
+                                                        i == Q_EMPTY || (i >= K_EMPTY && i < V_FULL) || (i >= V_EMPTY && i < S_FULL) || i == V_SEEN ? 2 : 1);
     ptx::fence_barrier_init();
   }
   if (warp == 10) {
@@ -320,6 +323,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           const int st = cnt % ST;
           if (cnt >= ST) ok = wait_all(bar(empty + st), (cnt / ST - 1) & 1);
           if (!ok) break;
+          if (!is_k && a.hold > 0 && (cnt & 1) == a.hold_odd)
+            for (const long long t0 = clock64(); clock64() - t0 < a.hold;) {}
           if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full + st), LY::KV_TILE);
           __syncwarp();
           if (lane < boxes) {
@@ -378,15 +383,26 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           }
           __syncwarp();
         };
-        ok = wait_all(bar(Q_FULL), q_cnt & 1) && (steps == 0 || k_here(0));
+        // In turns a stage waits for its own V tiles only, and behind an odd number of them the places of the ring change owner: the tile
+        // before in a place was then the other stage's.  While that one is still on its way, the phase that this stage would wait for
+        // looks like the one two before it, and the wait would pass at once.  So the stages tell each other when the last V tile of a
+        // piece is here, and nobody starts the next piece (its scores, from which the clearing of a tail follows, included) before.
+        // (K needs no such word: the queries that come first are loaded when all products with the ones before, and so with all K
+        // tiles before, are over.)
+        ok = wait_all(bar(Q_FULL), q_cnt & 1) && (q_cnt == 0 || wait_all(bar(V_SEEN), (q_cnt - 1) & 1)) && (steps == 0 || k_here(0));
         if (!ok) break;
         ptx::tc_fence_after();
         if (steps > 0) qk(0);
-        else if (lead) ptx::mbar_arrive(bar(Q_EMPTY));
+        else if (lead) {
+          ptx::mbar_arrive(bar(Q_EMPTY));
+          ptx::mbar_arrive(bar(V_SEEN));
+        }
         for (int i = 0; i < steps; ++i) {
           // Everything but P is waited for ahead, so that nothing stands between the last half of P and the next scores.
           const int c = tile_of(i), st = c % VST;
-          ok = wait_all(bar(V_FULL + st), (c / VST) & 1) && (i + 1 == steps || k_here(i + 1));
+          ok = wait_all(bar(V_FULL + st), (c / VST) & 1);
+          if (ok && i + 1 == steps && lead) ptx::mbar_arrive(bar(V_SEEN));
+          ok = ok && (i + 1 == steps || k_here(i + 1));
           // the first product of a unit overwrites O: its epilogue must have read the last one's
           if (ok && i == 0 && q_cnt > 0) ok = wait_all(bar(O_FREE + s), (q_cnt - 1) & 1);
 #pragma unroll
@@ -467,7 +483,8 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         ok = wait_all(bar(S_FULL + s), (it + i) & 1);      // (the stage's product with V of the step before is done as well)
         if (!ok) break;
         // Stale rows behind the cache's end must not meet P = 0 as NaN: they are cleared in the tile.  (Not before the wait above: the
-        // tile before in this place of the ring may not even have arrived, and the phase bit could not tell its load from this one's.)
+        // tile before in this place of the ring may not even have arrived, and the phase bit could not tell its load from this one's.  Behind it
+        // that tile is here: it was this stage's of the step before, or one of a piece before, see V_SEEN.)
         if (held < NT) {
           ok = wait_all(bar(V_FULL + c % VST), (c / VST) & 1);
           if (!ok) break;
@@ -883,6 +900,8 @@ cudaError_t launch_attend_chunk_sm100(const PagedDims& pd, const void* Q, const 
   a.cuts = reinterpret_cast<Cut*>(partials);
   a.partials = partials + (size_t)a.n_blocks * sizeof(Cut) / sizeof(float);
   a.sb = sb;
+  a.hold = test_hooks().hold_cycles;
+  a.hold_odd = test_hooks().hold_odd;
   CUtensorMap tq, tk, tv;
   if (!paged_q_map(&tq, pd, Q, a.TQ) || !paged_pool_map(&tk, pd, Kpool, pd.ks, a.box) || !paged_pool_map(&tv, pd, Vpool, pd.vs, a.box))
     return cudaErrorInvalidValue;

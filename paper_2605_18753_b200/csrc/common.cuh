@@ -295,6 +295,8 @@ void count_launch();
 struct TestHooks {
   long long wait_limit_cycles = 2000000000LL;   // how long a bounded device-side wait may spin (about 1 s)
   int skip_own_k_load = 0;                      // 1: the prefill attention kernel never loads its first K tile
+  long long hold_cycles = 0;                    // clocks that the chunk attention kernel holds back every other V tile
+  int hold_odd = 0;                             // ... the even ones (0) or the odd ones (1)
 };
 TestHooks& test_hooks();
 // Host-side checks shared by the entry points that live outside api.cu.
