@@ -332,6 +332,8 @@ typedef struct dash_rope {
 
 /* Rotates Q and K of a prefill shape (p->seq_q == p->seq_kv), or with inverse = 1 turns them back: the rotation is orthogonal,
  * so the backward pass is the inverse applied to the gradients.
+ *   p          batch, seq_q (at most 2^31 - 1 tokens in all), h_q, h_kv, head_dim, dtype, and q_stride / k_stride of the tensors that
+ *              are given; the rest (chunks, alpha, ...) is not read, so group sizes and lengths that the routing refuses are fine.
  *   positions  int32 [axes, batch, seq_q], contiguous.
  *   Q, Qout    by p->q_stride; K, Kout by p->k_stride (either pair may be NULL).  An output may be its own input; it may not
  *              overlap it otherwise, and output strides of 0 (broadcast) are refused. */

@@ -86,6 +86,24 @@ int make_rope(const dash_rope* r, int head_dim, RopeTable* rt) {
   return DASH_OK;
 }
 
+// A prefill shape as the rotation sees it: sizes, and the strides of the tensors that are given.  (Chunks, groups and the routing's
+// limits on them are none of its business.)
+int make_rope_dims(const dash_params* p, bool q, bool k, Dims* dm) {
+  if (!p || p->struct_size != sizeof(dash_params)) return DASH_ERR_INVALID_ARG;
+  if (p->batch <= 0 || p->batch > 65535 || p->seq_q <= 0 || p->seq_q != p->seq_kv || p->h_q <= 0 || p->h_kv <= 0) return DASH_ERR_INVALID_ARG;
+  if (p->h_q % p->h_kv != 0) return DASH_ERR_INVALID_ARG;
+  if (p->dtype != DASH_F32 && p->dtype != DASH_BF16) return DASH_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) return DASH_ERR_UNSUPPORTED;
+  if ((long long)p->batch * p->seq_q > 0x7fffffffLL) return DASH_ERR_UNSUPPORTED;      // (blocks of a grid)
+  std::memset(dm, 0, sizeof(*dm));
+  if ((q && !good_strides<3>(p->q_stride, p->dtype, dm->qs)) || (k && !good_strides<3>(p->k_stride, p->dtype, dm->ks)))
+    return DASH_ERR_INVALID_ARG;
+  dm->batch = p->batch; dm->seq_q = dm->seq_kv = p->seq_q;
+  dm->h_q = p->h_q; dm->h_kv = p->h_kv; dm->d = p->head_dim;
+  dm->dtype = p->dtype;
+  return DASH_OK;
+}
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t workspace_bytes(const PagedDims& pd) {
   const size_t partials = pd.dtype == DASH_BF16 ? chunk_sm100_partial_bytes(pd) : chunk_generic_partial_bytes(pd);
@@ -108,11 +126,11 @@ extern "C" {
 int dash_attn_rope(const dash_params* p, const dash_rope* rope, const int32_t* positions, const void* Q, const void* K,
                    void* Qout, void* Kout, int32_t inverse, void* stream) {
   Dims dm;
-  int rc = validate_params(p, &dm);
+  int rc = make_rope_dims(p, Q != nullptr, K != nullptr, &dm);
   if (rc != DASH_OK) return rc;
   RopeTable rt;
   if ((rc = make_rope(rope, dm.d, &rt)) != DASH_OK) return rc;
-  if (dm.decode || (inverse != 0 && inverse != 1)) return DASH_ERR_INVALID_ARG;
+  if (inverse != 0 && inverse != 1) return DASH_ERR_INVALID_ARG;
   if (!positions || !aligned4(positions) || (!Q && !K) || !Q != !Qout || !K != !Kout) return DASH_ERR_INVALID_ARG;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(Qout) || !aligned16(Kout)) return DASH_ERR_INVALID_ARG;
   if ((Q && broadcasts(dm.qs, dm.batch, dm.seq_q, dm.h_q)) || (K && broadcasts(dm.ks, dm.batch, dm.seq_q, dm.h_kv)))
