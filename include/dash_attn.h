@@ -320,14 +320,14 @@ typedef struct dash_paged_params {
 
 /* Rotary positions with 1 to 4 axes (time, height, width, ...).  Pair i of a head is turned by the angle
  * positions[axis[i]] * inv_freq[i]:  (x, y) -> (x cos - y sin, x sin + y cos).  The angle is formed as a 64-bit fraction of a
- * turn, so it is exact to 2^-32 turns at every int32 position.  Elements behind the pairs pass through. */
+ * turn, so it is within 2^-31 turns of the exact one at every int32 position.  Elements behind the pairs pass through. */
 typedef struct dash_rope {
   uint32_t struct_size;   /* sizeof(dash_rope); checked */
   int32_t pairs;          /* rotated pairs, 1 .. head_dim / 2 */
   int32_t axes;           /* rows of positions, 1 .. 4 */
   int32_t interleaved;    /* 0: pair i = elements (i, i + pairs); 1: elements (2i, 2i + 1) */
   const int32_t* axis;    /* host, pairs entries in [0, axes) */
-  const double* inv_freq; /* host, pairs entries: radians per position, finite */
+  const double* inv_freq; /* host, pairs entries: radians per position, at most 2^40 either way */
 } dash_rope;
 
 /* Rotates Q and K of a prefill shape (p->seq_q == p->seq_kv), or with inverse = 1 turns them back: the rotation is orthogonal,

@@ -61,14 +61,15 @@ bool pool_repeats(const PagedDims& pd, const long long* s, int num_pages) {
 }
 
 // Radians per position as a 64-bit fraction of a turn: x / 2 pi as an unevaluated sum of two doubles, each term's fraction in units of
-// 2^-64.  (In 80-bit arithmetic the 64 pairs of a head cost 3.6 us a call.)
+// 2^-64.  (In 80-bit arithmetic the 64 pairs of a head cost 3.6 us a call.)  Of the magnitude, the sign behind it: hi - floor(hi) is
+// exact for hi >= 0 only (1 - 1e-5 has no room for the last ten bits of 1e-5, and far positions multiply what is lost by 2^31).
+constexpr double MAX_FREQ = 1099511627776.0;      // 2^40: what the sum of two leaves out stays below 2^-64 there
 unsigned long long turn_fraction(double x) {
   constexpr double HI = 0.15915494309189535, LO = -9.839338337591243e-18;      // 1 / 2 pi
   constexpr double TWO64 = 18446744073709551616.0;
-  const double hi = x * HI, lo = std::fma(x, HI, -hi) + x * LO;
-  const double f = hi - std::floor(hi);
-  const double g = std::fabs(lo) < 0.25 ? lo : 0.0;        // (beyond 2^50 radians a position there is no fraction left in x itself)
-  return (f >= 1.0 ? 0ull : (unsigned long long)(f * TWO64)) + (unsigned long long)(long long)(g * TWO64);
+  const double m = std::fabs(x), hi = m * HI, lo = std::fma(m, HI, -hi) + m * LO;
+  const unsigned long long f = (unsigned long long)((hi - std::floor(hi)) * TWO64) + (unsigned long long)(long long)(lo * TWO64);
+  return x < 0 ? 0ull - f : f;
 }
 
 int make_rope(const dash_rope* r, int head_dim, RopeTable* rt) {
@@ -79,7 +80,7 @@ int make_rope(const dash_rope* r, int head_dim, RopeTable* rt) {
   rt->pairs = r->pairs;
   rt->interleaved = r->interleaved;
   for (int i = 0; i < r->pairs; ++i) {
-    if (r->axis[i] < 0 || r->axis[i] >= r->axes || !std::isfinite(r->inv_freq[i])) return DASH_ERR_INVALID_ARG;
+    if (r->axis[i] < 0 || r->axis[i] >= r->axes || !(std::fabs(r->inv_freq[i]) <= MAX_FREQ)) return DASH_ERR_INVALID_ARG;
     rt->axis[i] = (unsigned char)r->axis[i];
     rt->freq[i] = turn_fraction(r->inv_freq[i]);
   }

@@ -2,9 +2,9 @@
 //
 // Pair i of a head turns by theta = pos[axis(i)] f_i.  In fp32 the product has no fraction left at a far position, so the angle
 // is formed in turns as a 64-bit fixed-point fraction: (f_i / 2 pi mod 1) 2^64, multiplied by the position modulo 2^64.  Dropped
-// whole turns wrap by themselves and the fraction is exact to the position times 2^-64; its upper 32 bits are kept.  Two more
-// bits give the quadrant, the rest lies within an eighth of a turn, where Taylor polynomials (sine to x^9, cosine to x^10)
-// are within 2e-9 of the functions.
+// whole turns wrap by themselves and the fraction is exact to the position times 2^-64; its upper 32 bits are kept (2^-31 turns in
+// all).  Two more bits give the quadrant, the rest lies within an eighth of a turn, where Taylor polynomials (sine to x^9, cosine
+// to x^10) are within 2e-9 of the functions.
 //
 // Memory-bound: every element is read and written once.  A thread owns one piece of the head (N pairs: two 16-byte vectors) of one
 // token, forms its cosines and sines in registers and takes the piece through its share of the heads, four heads on their way

@@ -60,3 +60,10 @@ def test_strides_of_an_absent_tensor_do_not_matter(lib):
     bad = _p()
     bad.struct_size = 8
     assert _call(lib, bad, 16, 16, 16, 16, 16, 0) == -1
+
+
+@pytest.mark.parametrize("freq,code", [(2.0 ** 40, None), (-2.0 ** 40, None), (2.0 ** 40 * (1 + 2.0 ** -52), -1), (-1e300, -1),
+                                       (float("inf"), -1), (float("nan"), -1), (0.0, None), (-1e-300, None)])
+def test_frequencies_whose_fraction_is_lost_are_refused(lib, freq, code):
+    got = lib.dash_attn_rope(ctypes.byref(_p()), ctypes.byref(B.make_rope([1.0, freq])), 16, 16, 16, 16, 16, 0, None)
+    assert got == code if code else got not in (-1, -2, -3)
