@@ -385,6 +385,7 @@ int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const vo
  * up to `keep` in all, the slots in between with the largest mass (equal mass: the lower slot; NaN counts as less than
  * everything).  The kept tokens move to slots 0, 1, ... in their old order.  Shorter sequences keep everything.
  *   mass      fp32 [batch, h_kv, max_pages * page_size] (read below kv_len).
+ *   keep      at most 2^30.
  *   kept      int32 [batch, h_kv, keep], output: old slots, ascending; -1 behind the new length.
  *   new_len   int32 [batch], output: min(kv_len, keep); may not be kv_len itself.
  *   Kdst, Vdst, dst_table, dst_max_pages, dst_num_pages   where the kept rows go: pools with the strides of Kpool / Vpool, page

@@ -222,6 +222,7 @@ int dash_attn_evict_paged(const dash_paged_params* p, int32_t keep, int32_t sink
   int rc = make_paged(p, &pd);
   if (rc != DASH_OK) return rc;
   if (keep <= 0 || sinks < 0 || recent < 0 || (long long)sinks + recent > keep) return DASH_ERR_INVALID_ARG;
+  if (keep > (1 << 30)) return DASH_ERR_UNSUPPORTED;       // (a block's steps through `kept` stay within 32 bits)
   if (!mass || !kv_len || !page_table || !Kpool || !Vpool || !kept || !new_len || !dst_table || !Kdst || !Vdst) return DASH_ERR_INVALID_ARG;
   if (dst_max_pages <= 0 || dst_num_pages <= 0) return DASH_ERR_INVALID_ARG;
   const long long dst_cap = (long long)dst_max_pages * pd.page_size;
