@@ -434,9 +434,45 @@ _I32, _F32 = torch.int32, torch.float32
 _TORCH_DTYPE = (torch.float32, torch.bfloat16)        # by dash_dtype
 
 
-def _refuse(where, dtype, ints, floats, tensors):
+class _Layout:
+    """Sizes, shapes and strides that the parameters say, worked out once per set of values (the parameters keep them beside a copy of
+    the values they come from, so a change shows)."""
+    __slots__ = ("raw", "dtype", "batch", "rows", "entries", "sums", "groups", "slots", "q", "o", "kn", "vn", "k", "v")
+
+    def __init__(self, p, raw):
+        self.raw, self.dtype, d = raw, _TORCH_DTYPE[p.dtype], p.head_dim
+        if isinstance(p, DashPagedParams):
+            self.batch, self.rows, self.entries, self.sums = p.batch, p.rows, p.batch * p.max_pages, p.rows * p.h_q
+            self.groups, self.slots = p.batch * p.h_kv, p.batch * p.h_kv * p.max_pages * p.page_size
+            self.q, self.o = (((p.rows, p.h_q, d), (*s, 1)) for s in (p.q_stride, p.o_stride))
+            self.kn, self.vn = (((p.rows, p.h_kv, d), (*s, 1)) for s in (p.kn_stride, p.vn_stride))
+            self.k, self.v = (((p.num_pages, p.page_size, p.h_kv, d), (*s, 1)) for s in (p.k_stride, p.v_stride))
+        else:
+            self.q, self.k = (((p.batch, p.seq_q, h, d), (*s, 1)) for h, s in ((p.h_q, p.q_stride), (p.h_kv, p.k_stride)))
+
+
+def _layout(p):
+    raw, got = bytes(p), p.__dict__.get("_layout")
+    if got is None or got.raw != raw:
+        got = p._layout = _Layout(p, raw)
+    return got
+
+
+def _misfits(where, **pairs):
+    """Raises for the tensors that do not have the parameters' shape and strides (the stride of a dimension of one element says
+    nothing, and an empty tensor's none)."""
+    for name, (t, (shape, stride)) in pairs.items():
+        if t is None:
+            continue
+        if t.shape != shape or t.numel() > 0 and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), stride)):
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)} with strides {t.stride()}, the parameters say {shape} with strides {stride}")
+
+
+def _refuse(where, dtype, ints, floats, tensors, workspace=None):
     """Says which argument the kernels would misread: they take index tensors as contiguous int32, lse and mass as contiguous fp32,
-    queries, keys and values in the parameters' dtype, all on the current device."""
+    queries, keys and values in the parameters' dtype, all on the current device, as is the workspace."""
+    if workspace is not None and not (workspace.get_device() == torch._C._cuda_getDevice() and workspace.is_contiguous()):
+        raise ValueError(f"{where}: expected a contiguous workspace on the current device, got one on {workspace.device} with strides {workspace.stride()}")
     for kind, want, ts in (("int32", _I32, ints), ("float32", _F32, floats), ("", dtype, tensors)):
         for t in ts:
             if t is None:
@@ -456,21 +492,20 @@ def _sizes(where, **pairs):
 
 def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
     """Q and K (either may be None) of a prefill shape rotated; inverse=True turns them back, which is the backward pass when it is
-    given the gradients.  positions int32 [axes, batch, seq]; outputs have the strides of their inputs and may be them."""
-    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    given the gradients.  positions int32 [axes, batch, seq]; inputs and outputs have the parameters' strides, and an output may be its input."""
+    dev, lay = torch._C._cuda_getDevice(), _layout(p)
+    dt = lay.dtype
     if not (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()):
         _refuse("dash_attn_rope", dt, (positions,), (), ())
-    for x, y, h in ((Q, Qout, p.h_q), (K, Kout, p.h_kv)):
+    for x, y, (shape, stride) in ((Q, Qout, lay.q), (K, Kout, lay.k)):
         if x is None and y is None:
             continue
         if x is None or y is None:
             raise ValueError("dash_attn_rope: every input has an output")
         if not (x.dtype is dt and y.dtype is dt and x.get_device() == dev and y.get_device() == dev):
             _refuse("dash_attn_rope", dt, (), (), (x, y))
-        if x.shape != (p.batch, p.seq_q, h, p.head_dim) or x.shape != y.shape:
-            raise ValueError("dash_attn_rope: tensors are [batch, seq, heads, head_dim] of the parameters, an output like its input")
-        if x is not y and not (x.is_contiguous() and y.is_contiguous()) and x.stride() != y.stride():
-            raise ValueError("dash_attn_rope: an output has the strides of its input")
+        if not (x.shape == shape and x.stride() == stride and (x is y or y.shape == shape and y.stride() == stride)):
+            _misfits("dash_attn_rope", input=(x, (shape, stride)), output=(y, (shape, stride)))
     if positions.numel() != rope.axes * p.batch * p.seq_q:
         raise ValueError("positions must be [axes, batch, seq]")
     rc = (_lib or lib()).dash_attn_rope(ctypes.byref(p), ctypes.byref(rope), positions.data_ptr(), Q if Q is None else Q.data_ptr(),
@@ -483,7 +518,8 @@ def dash_attn_rope(p, rope, positions, Q, K, Qout, Kout, inverse=False):
 def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Qout, K, V, Kpool, Vpool):
     """Packed new tokens into their pages: K rotated, V as it is, Q rotated into Qout (Q and Qout None: keys and values only;
     rope and positions None: no rotation)."""
-    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    dev, lay = torch._C._cuda_getDevice(), _layout(p)
+    dt = lay.dtype
     if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and K.dtype is dt and V.dtype is dt
             and Kpool.dtype is dt and Vpool.dtype is dt and q_start.get_device() == dev and kv_len.get_device() == dev
             and page_table.get_device() == dev and K.get_device() == dev and V.get_device() == dev and Kpool.get_device() == dev
@@ -491,14 +527,15 @@ def dash_attn_append_paged(p, rope, positions, q_start, kv_len, page_table, Q, Q
             and (positions is None or (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous()))
             and (Q is None or (Q.dtype is dt and Q.get_device() == dev)) and (Qout is None or (Qout.dtype is dt and Qout.get_device() == dev))):
         _refuse("dash_attn_append_paged", dt, (positions, q_start, kv_len, page_table), (), (Q, Qout, K, V, Kpool, Vpool))
-    n, rows = p.batch, p.rows
-    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
-            and Vpool.size(0) == p.num_pages and K.size(0) == rows and V.size(0) == rows and (Q is None or Q.size(0) == rows)
-            and (Qout is None or Qout.size(0) == rows)):
+    n, rows = lay.batch, lay.rows
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == lay.entries):
         _sizes("dash_attn_append_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
-               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages),
-               K=(K.size(0), rows), V=(V.size(0), rows), Q=(rows if Q is None else Q.size(0), rows),
-               Qout=(rows if Qout is None else Qout.size(0), rows))
+               page_table=(page_table.numel(), lay.entries))
+    if not (K.shape == lay.kn[0] and K.stride() == lay.kn[1] and V.shape == lay.vn[0] and V.stride() == lay.vn[1]
+            and Kpool.shape == lay.k[0] and Kpool.stride() == lay.k[1] and Vpool.shape == lay.v[0] and Vpool.stride() == lay.v[1]
+            and (Q is None or (Q.shape == lay.q[0] and Q.stride() == lay.q[1]))
+            and (Qout is None or (Qout.shape == lay.o[0] and Qout.stride() == lay.o[1]))):
+        _misfits("dash_attn_append_paged", Q=(Q, lay.q), Qout=(Qout, lay.o), K=(K, lay.kn), V=(V, lay.vn), Kpool=(Kpool, lay.k), Vpool=(Vpool, lay.v))
     if (rope is None) != (positions is None):
         raise ValueError("dash_attn_append_paged: rope and positions come together")
     if positions is not None and positions.numel() != rope.axes * rows:
@@ -528,19 +565,23 @@ def alloc_paged_workspace(p: DashPagedParams, device="cuda") -> torch.Tensor:
 
 def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len, O, lse, workspace):
     """Dense causal attention of packed new tokens over their sequences' pages; lse (None to skip) fp32 [rows, h_q]."""
-    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    dev, lay = torch._C._cuda_getDevice(), _layout(p)
+    dt = lay.dtype
     if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and Q.dtype is dt and O.dtype is dt
             and Kpool.dtype is dt and Vpool.dtype is dt and q_start.get_device() == dev and kv_len.get_device() == dev
             and page_table.get_device() == dev and Q.get_device() == dev and O.get_device() == dev and Kpool.get_device() == dev
             and Vpool.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
+            and workspace.get_device() == dev and workspace.is_contiguous()
             and (lse is None or (lse.dtype is _F32 and lse.get_device() == dev and lse.is_contiguous()))):
-        _refuse("dash_attn_attend_chunk_paged", dt, (page_table, q_start, kv_len), (lse,), (Q, Kpool, Vpool, O))
-    n, rows = p.batch, p.rows
-    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
-            and Vpool.size(0) == p.num_pages and Q.size(0) == rows and O.size(0) == rows and (lse is None or lse.numel() == rows * p.h_q)):
+        _refuse("dash_attn_attend_chunk_paged", dt, (page_table, q_start, kv_len), (lse,), (Q, Kpool, Vpool, O), workspace)
+    n = lay.batch
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == lay.entries
+            and (lse is None or lse.numel() == lay.sums)):
         _sizes("dash_attn_attend_chunk_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
-               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages),
-               Q=(Q.size(0), rows), O=(O.size(0), rows), lse=(rows * p.h_q if lse is None else lse.numel(), rows * p.h_q))
+               page_table=(page_table.numel(), lay.entries), lse=(lay.sums if lse is None else lse.numel(), lay.sums))
+    if not (Q.shape == lay.q[0] and Q.stride() == lay.q[1] and O.shape == lay.o[0] and O.stride() == lay.o[1]
+            and Kpool.shape == lay.k[0] and Kpool.stride() == lay.k[1] and Vpool.shape == lay.v[0] and Vpool.stride() == lay.v[1]):
+        _misfits("dash_attn_attend_chunk_paged", Q=(Q, lay.q), O=(O, lay.o), Kpool=(Kpool, lay.k), Vpool=(Vpool, lay.v))
     rc = (_lib or lib()).dash_attn_attend_chunk_paged(
         ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
         O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
@@ -551,22 +592,23 @@ def dash_attn_attend_chunk_paged(p, Q, Kpool, Vpool, page_table, q_start, kv_len
 
 def dash_attn_key_mass_paged(p, Q, Kpool, page_table, q_start, kv_len, lse, mass_in, mass_out, workspace, decay=1.0):
     """Weights that the new rows give every cached token, added to decay * mass_in (None: zeros); fp32 [batch, h_kv, slots]."""
-    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    dev, lay = torch._C._cuda_getDevice(), _layout(p)
+    dt = lay.dtype
     if not (q_start.dtype is _I32 and kv_len.dtype is _I32 and page_table.dtype is _I32 and Q.dtype is dt and Kpool.dtype is dt
             and lse.dtype is _F32 and mass_out.dtype is _F32 and q_start.get_device() == dev and kv_len.get_device() == dev
             and page_table.get_device() == dev and Q.get_device() == dev and Kpool.get_device() == dev and lse.get_device() == dev
             and mass_out.get_device() == dev and q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
-            and lse.is_contiguous() and mass_out.is_contiguous()
+            and lse.is_contiguous() and mass_out.is_contiguous() and workspace.get_device() == dev and workspace.is_contiguous()
             and (mass_in is None or (mass_in.dtype is _F32 and mass_in.get_device() == dev and mass_in.is_contiguous()))):
-        _refuse("dash_attn_key_mass_paged", dt, (page_table, q_start, kv_len), (lse, mass_in, mass_out), (Q, Kpool))
-    n, slots = p.batch, p.batch * p.h_kv * p.max_pages * p.page_size
-    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == n * p.max_pages and Kpool.size(0) == p.num_pages
-            and Q.size(0) == p.rows and lse.numel() == p.rows * p.h_q and mass_out.numel() == slots
-            and (mass_in is None or mass_in.numel() == slots)):
+        _refuse("dash_attn_key_mass_paged", dt, (page_table, q_start, kv_len), (lse, mass_in, mass_out), (Q, Kpool), workspace)
+    n, slots = lay.batch, lay.slots
+    if not (q_start.numel() == n + 1 and kv_len.numel() == n and page_table.numel() == lay.entries and lse.numel() == lay.sums
+            and mass_out.numel() == slots and (mass_in is None or mass_in.numel() == slots)):
         _sizes("dash_attn_key_mass_paged", q_start=(q_start.numel(), n + 1), kv_len=(kv_len.numel(), n),
-               page_table=(page_table.numel(), n * p.max_pages), Kpool=(Kpool.size(0), p.num_pages), Q=(Q.size(0), p.rows),
-               lse=(lse.numel(), p.rows * p.h_q), mass_in=(slots if mass_in is None else mass_in.numel(), slots),
-               mass_out=(mass_out.numel(), slots))
+               page_table=(page_table.numel(), lay.entries), lse=(lse.numel(), lay.sums),
+               mass_in=(slots if mass_in is None else mass_in.numel(), slots), mass_out=(mass_out.numel(), slots))
+    if not (Q.shape == lay.q[0] and Q.stride() == lay.q[1] and Kpool.shape == lay.k[0] and Kpool.stride() == lay.k[1]):
+        _misfits("dash_attn_key_mass_paged", Q=(Q, lay.q), Kpool=(Kpool, lay.k))
     rc = (_lib or lib()).dash_attn_key_mass_paged(
         ctypes.byref(p), Q.data_ptr(), Kpool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), lse.data_ptr(),
         decay, None if mass_in is None else mass_in.data_ptr(), mass_out.data_ptr(), workspace.data_ptr(), workspace.numel(),
@@ -579,7 +621,8 @@ def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_l
                           sinks=0, recent=0):
     """Keeps `keep` tokens of every (sequence, KV head) and moves them to the front of the destination pages (page_table, Kpool,
     Vpool themselves for in place)."""
-    dev, dt = torch._C._cuda_getDevice(), _TORCH_DTYPE[p.dtype]
+    dev, lay = torch._C._cuda_getDevice(), _layout(p)
+    dt = lay.dtype
     if not (kv_len.dtype is _I32 and page_table.dtype is _I32 and kept.dtype is _I32 and new_len.dtype is _I32 and dst_table.dtype is _I32
             and mass.dtype is _F32 and Kpool.dtype is dt and Vpool.dtype is dt and Kdst.dtype is dt and Vdst.dtype is dt
             and kv_len.get_device() == dev and page_table.get_device() == dev and kept.get_device() == dev and new_len.get_device() == dev
@@ -588,20 +631,19 @@ def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_l
             and kept.is_contiguous() and new_len.is_contiguous() and dst_table.is_contiguous() and mass.is_contiguous()
             and (mass_out is None or (mass_out.dtype is _F32 and mass_out.get_device() == dev and mass_out.is_contiguous()))):
         _refuse("dash_attn_evict_paged", dt, (kv_len, page_table, kept, new_len, dst_table), (mass, mass_out), (Kpool, Vpool, Kdst, Vdst))
-    n, groups, shape = p.batch, p.batch * p.h_kv, Kdst.shape
+    n, groups, shape, page = lay.batch, lay.groups, Kdst.shape, lay.k[0][1]
     width = dst_table.size(-1)
-    if not (kv_len.numel() == n and new_len.numel() == n and page_table.numel() == n * p.max_pages and dst_table.numel() == n * width
-            and kept.numel() == groups * keep and mass.numel() == groups * p.max_pages * p.page_size
-            and (mass_out is None or mass_out.numel() == groups * width * p.page_size) and Kpool.size(0) == p.num_pages
-            and Vpool.size(0) == p.num_pages and Vdst.shape == shape):
-        slots, out = groups * p.max_pages * p.page_size, groups * width * p.page_size
+    if not (kv_len.numel() == n and new_len.numel() == n and page_table.numel() == lay.entries and dst_table.numel() == n * width
+            and kept.numel() == groups * keep and mass.numel() == lay.slots
+            and (mass_out is None or mass_out.numel() == groups * width * page) and Vdst.shape == shape):
+        out = groups * width * page
         _sizes("dash_attn_evict_paged", kv_len=(kv_len.numel(), n), new_len=(new_len.numel(), n),
-               page_table=(page_table.numel(), n * p.max_pages), dst_table=(dst_table.numel(), n * width), kept=(kept.numel(), groups * keep),
-               mass=(mass.numel(), slots), mass_out=(out if mass_out is None else mass_out.numel(), out),
-               Kpool=(Kpool.size(0), p.num_pages), Vpool=(Vpool.size(0), p.num_pages), Vdst=(tuple(Vdst.shape), tuple(shape)))
-    if shape[1:] != Kpool.shape[1:] or not (Kdst.is_contiguous() and Kpool.is_contiguous() or Kdst.stride() == Kpool.stride()) \
-            or not (Vdst.is_contiguous() and Vpool.is_contiguous() or Vdst.stride() == Vpool.stride()):
-        raise ValueError("dash_attn_evict_paged: the destination pools must have the pools' page size, heads and strides")
+               page_table=(page_table.numel(), lay.entries), dst_table=(dst_table.numel(), n * width), kept=(kept.numel(), groups * keep),
+               mass=(mass.numel(), lay.slots), mass_out=(out if mass_out is None else mass_out.numel(), out), Vdst=(tuple(Vdst.shape), tuple(shape)))
+    if not (Kpool.shape == lay.k[0] and Kpool.stride() == lay.k[1] and Vpool.shape == lay.v[0] and Vpool.stride() == lay.v[1]
+            and shape[1:] == lay.k[0][1:] and Kdst.stride() == lay.k[1] and Vdst.stride() == lay.v[1]):
+        to = (shape[0], *lay.k[0][1:])         # the destination's pages: as many as there are, of the pools' size, heads and strides
+        _misfits("dash_attn_evict_paged", Kpool=(Kpool, lay.k), Vpool=(Vpool, lay.v), Kdst=(Kdst, (to, lay.k[1])), Vdst=(Vdst, (to, lay.v[1])))
     rc = (_lib or lib()).dash_attn_evict_paged(
         ctypes.byref(p), keep, sinks, recent, mass.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(),
         kept.data_ptr(), new_len.data_ptr(), dst_table.data_ptr(), width, shape[0], Kdst.data_ptr(), Vdst.data_ptr(),
