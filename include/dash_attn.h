@@ -415,12 +415,14 @@ int64_t dash_attn_launch_count(void);
 
 /* Switches for the test-suite; production code never calls this (process-wide, not thread-safe, defaults restored
  * by (0, 0)).
- *   wait_limit_cycles  SM clock cycles a bounded device-side wait of the prefill attention kernel may spin before it
- *                      gives up with DASH_ERR_TIMEOUT; <= 0 restores the default (2e9, about a second).
+ *   wait_limit_cycles  SM clock cycles a bounded device-side wait of the prefill attention kernel (and of the bf16 chunk
+ *                      attention and key mass kernels) may spin before it gives up with DASH_ERR_TIMEOUT; <= 0 restores
+ *                      the default (2e9, about a second).
  *   skip_own_k_load    1: the tensor-core prefill attention kernel never issues the load of its first K tile, so
  *                      the waits for it run out -- with a short limit this exercises the time-out path (roles leave
  *                      their loops, copies in flight land, tensor memory is freed, the status word is set) without
- *                      hanging or faulting anything. */
+ *                      hanging or faulting anything.  The chunk attention kernel leaves out the fourth K tile of each
+ *                      block, the key mass kernel the keys of its second unit of 256 slots, with work in flight. */
 void dash_attn_test_hooks(int64_t wait_limit_cycles, int32_t skip_own_k_load);
 
 /* The same kind of switch for the bf16 dash_attn_attend_chunk_paged: its loader holds back every other tile of values (the

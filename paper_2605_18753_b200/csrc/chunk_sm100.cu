@@ -91,6 +91,8 @@ struct ChunkArgs {
   StatusBlock* sb;
   long long hold;                  // test hook: clocks that V tiles of one parity are held back (0: none)
   int hold_odd;
+  int inject;                      // test hook: the fourth K tile of a block is never loaded (the waits for it run out)
+  long long wait_limit;            // clocks that a bounded wait may spin
 };
 
 // One block's share of a unit.
@@ -211,7 +213,7 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
   const uint32_t sbase = ptx::smem_u32(smem);
   auto bar = [&](int i) { return ptx::smem_u32(&misc->bar[i]); };
   volatile int* abort_flag = &misc->abort_flag;
-  auto wait_all = [&](uint32_t barrier, uint32_t parity) { return ptx::mbar_wait_warp(barrier, parity, abort_flag); };
+  auto wait_all = [&](uint32_t barrier, uint32_t parity) { return ptx::mbar_wait_warp(barrier, parity, abort_flag, a.wait_limit); };
   const int g_q = pd.g_q, TQ = a.TQ, TT = 2 * TQ;
 
   if (tid == 0) {
@@ -312,6 +314,10 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         }
         const int* table = a.page_table + (long long)p.b * pd.max_pages;
         for (int j = 0; j < p.len && ok; ++j, ++cnt) {
+          if (is_k && a.inject && cnt == 3) {
+            ok = false;
+            break;
+          }
           const int slot = (p.k0 + j) * NT + lane * a.box;
           int page = pd.num_pages, tok = 0;   // (out of range: the box is filled with zeros)
           if (lane < boxes && slot < p.s.valid) {
@@ -902,6 +908,8 @@ cudaError_t launch_attend_chunk_sm100(const PagedDims& pd, const void* Q, const 
   a.sb = sb;
   a.hold = test_hooks().hold_cycles;
   a.hold_odd = test_hooks().hold_odd;
+  a.inject = test_hooks().skip_own_k_load;
+  a.wait_limit = test_hooks().wait_limit_cycles;
   CUtensorMap tq, tk, tv;
   if (!paged_q_map(&tq, pd, Q, a.TQ) || !paged_pool_map(&tk, pd, Kpool, pd.ks, a.box) || !paged_pool_map(&tv, pd, Vpool, pd.vs, a.box))
     return cudaErrorInvalidValue;

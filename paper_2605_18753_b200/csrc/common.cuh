@@ -294,7 +294,7 @@ void count_launch();
 // Host-side switches for the tests (set through dash_attn_test_hooks; the defaults are what production runs with).
 struct TestHooks {
   long long wait_limit_cycles = 2000000000LL;   // how long a bounded device-side wait may spin (about 1 s)
-  int skip_own_k_load = 0;                      // 1: the prefill attention kernel never loads its first K tile
+  int skip_own_k_load = 0;                      // 1: the prefill attention kernel never loads its first K tile (chunk attention: fourth; key mass: second unit)
   long long hold_cycles = 0;                    // clocks that the chunk attention kernel holds back every other V tile
   int hold_odd = 0;                             // ... the even ones (0) or the odd ones (1)
 };

@@ -75,6 +75,8 @@ struct MassArgs {
   float* parts;                    // [block][place][256]: place 0 a unit begun by an earlier block, 1 one that later blocks go on with
   struct MassCut* cuts;
   StatusBlock* sb;
+  int inject;                      // test hook: the keys of a block's second unit are never loaded (the waits for them run out)
+  long long wait_limit;            // clocks that a bounded wait may spin
 };
 
 struct MassCut {                   // the unit that a block cuts at its end
@@ -211,7 +213,7 @@ key_mass_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   const uint32_t sbase = ptx::smem_u32(smem);
   auto bar = [&](int i) { return ptx::smem_u32(&misc->bar[i]); };
   volatile int* abort_flag = &misc->abort_flag;
-  auto wait_all = [&](uint32_t barrier, uint32_t parity) { return ptx::mbar_wait_warp(barrier, parity, abort_flag); };
+  auto wait_all = [&](uint32_t barrier, uint32_t parity) { return ptx::mbar_wait_warp(barrier, parity, abort_flag, a.wait_limit); };
   const int g_q = pd.g_q, QT = a.QT;
 
   if (tid == 0) {
@@ -281,6 +283,7 @@ key_mass_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     for (; ok && !walk.done(); walk.next(a, pref)) {
       const Unit x(a, walk);
       if (x.t0 >= x.t1) continue;
+      if (a.inject && kc == 1) break;
       const int* table = a.page_table + (long long)x.b * pd.max_pages;
       const int slot = x.slot0 + lane * a.box;
       int page = pd.num_pages, tok = 0;      // (out of range: zeros)
@@ -540,6 +543,8 @@ cudaError_t launch_key_mass_sm100(const PagedDims& pd, const void* Q, const void
   a.cuts = reinterpret_cast<MassCut*>(partials);
   a.parts = partials + (size_t)current_sm_count() * sizeof(MassCut) / sizeof(float);
   a.sb = sb;
+  a.inject = test_hooks().skip_own_k_load;
+  a.wait_limit = test_hooks().wait_limit_cycles;
   CUtensorMap tq, tk;
   if (!paged_pool_map(&tk, pd, Kpool, pd.ks, a.box)) return cudaErrorInvalidValue;
   PagedDims pq = pd;
