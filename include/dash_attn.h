@@ -395,7 +395,8 @@ int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const vo
  *   mass_out  fp32 [batch, h_kv, dst_max_pages * page_size]: the mass of the kept tokens at their new slots, NULL to skip; may be
  *             mass itself in place.
  * Slots at and behind the new length are left as they are.  Chunk summaries of a cache that has moved are stale:
- * dash_attn_block_summaries_paged makes them anew.  p->rows, p->h_q and the strides of packed tensors are not used. */
+ * dash_attn_block_summaries_paged makes them anew.  p->rows, p->h_q and the strides of packed tensors have to be
+ * valid (strides of 0 are), but are not used. */
 int dash_attn_evict_paged(const dash_paged_params* p, int32_t keep, int32_t sinks, int32_t recent, const float* mass,
                           const int32_t* kv_len, const int32_t* page_table, const void* Kpool, const void* Vpool,
                           int32_t* kept, int32_t* new_len, const int32_t* dst_table, int32_t dst_max_pages,
