@@ -376,6 +376,8 @@ int dash_attn_attend_chunk_paged(const dash_paged_params* p, const void* Q, cons
  *   Rows with lse -inf give no weight; queries are taken to be finite (a NaN in one reaches every slot that the row sees, and may
  *   reach others of its tile).
  *   decay     finite; 1 accumulates.
+ * fp32 sums; bf16 calls with many rows take a quarter of the exponentials from a polynomial of relative error 2.9e-6 (the mass of
+ * 2048 rows over 8192 slots is then off by 1.8e-7 in the 2-norm, by 9.4e-8 without).
  * No atomics: every sum has one owner and one order.  Workspace as above (its status word is used). */
 int dash_attn_key_mass_paged(const dash_paged_params* p, const void* Q, const void* Kpool, const int32_t* page_table,
                              const int32_t* q_start, const int32_t* kv_len, const float* lse, float decay,

@@ -350,7 +350,11 @@ __global__ void __launch_bounds__(THREADS, 2) key_mass_generic_kernel(const __gr
   }
 }
 
-// Rows per tile: 16 where the sequences have fewer than 32 rows on average (64 x 64 tiles would be mostly empty), else 64.
+// Rows per tile: 16 where the sequences have fewer than 32 rows on average (64 x 64 tiles would be mostly empty), else 64.  Eight caches
+// of 4096, 8/2 heads, d 64, tiles of 16 | 64 rows, attention and weights: 1 token (4 rows) 31 | 35 and 21 | 27 us, 4 tokens 61 | 45 and
+// 27 | 29, 7 tokens 81 | 45 and 33 | 31, 8 tokens 80 | 51 and 35 | 31: the weights' line is where it belongs, the attention's would be
+// lower, at about 12 rows.  A prompt among single tokens has the tiles of the average: 63 and one of 256 over 2048 slots 148 | 227
+// and 233 | 162, 31 and one of 512 (d 128) 442 | 279 and 705 | 252.
 int rows_per_tile(const PagedDims& pd) { return (long long)pd.rows * pd.g_q < 32LL * pd.batch ? 16 : 64; }
 long long row_slots(const PagedDims& pd) { return (long long)pd.rows * pd.g_q / rows_per_tile(pd) + pd.batch; }
 

@@ -21,13 +21,15 @@
 // weights held up the other's scores).  P is written over S in tensor memory (bf16) and is the A operand of P V; its first three
 // quarters go to the product while the last is formed.
 //
-// What bounds it: 4096 rows over 16384 slots, 32/8 heads, d 128 (962 GFLOP): 765 us, 1.26 PFLOP/s, 75 % of the measured cuBLAS burst
-// (in a long loop the power limit holds it at 0.89 ms); the same schedule without the softmax arithmetic takes 608 us, without
-// all but one MMA of each product 665, so the softmax threads' chain of a step (scores out of tensor memory, maximum, 128
+// What bounds it: 4096 rows over 16384 slots, 32/8 heads, d 128 (962 GFLOP): 0.88 to 0.90 ms in a long loop, 1.08 PFLOP/s, 78 % of the
+// measured sustained cuBLAS rate (the power limit; the first calls of a cool GPU take 765 us, 75 % of the burst).  Of those 765, the
+// same schedule without the softmax arithmetic takes 608 us, without all but one MMA of each product 665, so the softmax threads' chain of a step (scores out of tensor memory, maximum, 128
 // exponentials, weights back) is the longer of the two.  Tried and slower: steps of 64 slots with two score buffers (the scores'
 // products then read Q from shared memory twice as often), two warpgroups per stage (1.18 ms: 96 registers a thread), the weights
-// formed ahead of the maximum.  One token of each of 16 caches of up to 65536 slots (2.4 GB): 378 us, 6.4 TB/s, 97 % of the measured
-// copy.
+// formed ahead of the maximum.  One token of each of 16 caches of up to 65536 slots (2.4 GB): 371 to 421 us
+// by GPU, 5.7 to 6.5 TB/s, 87 to 99 % of the measured copy.
+// Rounding: the weights meet V as one bf16 term (2^-8 of each at most, against their unrounded sum), because a second term would be half of
+// the products again.  O against float64 (2-norm): 2.3e-3, of which its own rounding to bf16 is 1.7e-3.
 // Every wait is bounded; one that runs out raises DASH_ERR_TIMEOUT in the status word, and every role leaves.
 #include <cuda.h>
 
@@ -726,7 +728,9 @@ attend_chunk_sm100_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
 }
 
 // Joins the partial results of a cut unit: block (x, y) the unit that attention block x cuts at its end, its y-th share.
-//   a unit of two row tiles (in few parts): 32 columns of all rows, a row per thread;
+//   a unit of two row tiles: 32 columns of all rows, a row per thread, part after part (few where there are many such units; where one is
+//   all there is, the parts are a chain: 32 and 33 tokens over 65536 slots, 4 heads on one KV head, 78 and 193 us in all, with 8 KV
+//   heads 84 and 104);
 //   fewer rows (in up to 2 x 148 parts, where one long cache is all there is): a share of the rows, a thread four columns of one,
 //   neighbouring threads neighbouring rows (as the parts lie), and what is left of the threads as P groups that take every P-th part and
 //   meet in shared memory, so that a hundred parts are no chain of a hundred loads (16 tokens over 27,000 slots: 34 us in all, 73

@@ -12,7 +12,9 @@
 // Move (evict_move_kernel): bytes.  To other pages: blocks along the kept rows (4096 of each of 128 caches, 537 MB read and written: 94 us,
 // 5.7 TB/s, 87 % of the measured copy).  In place: row j comes from slot kept[j] >= j, so one
 // block that takes the rows in order, each batch in registers before any of it is written, never writes a row that it has yet
-// to read; a (sequence, KV head) is divided among blocks by 64-byte columns of K and V instead, which nobody else touches.
+// to read; a (sequence, KV head) is divided among blocks by 64-byte columns of K and V instead, which nobody else touches.  16 x 8
+// caches of 32768 slots to 4096, d 128, bf16: 191 us with the selection, 84 us of bytes (the rows of a batch wait for each other); of 4196 slots
+// 172; caches that are not above the limit are written onto themselves (4096 slots: 158).
 #include "paged.cuh"
 #include "sm100_ptx.cuh"
 

@@ -10,7 +10,9 @@
 // token, forms its cosines and sines in registers and takes the piece through its share of the heads, four heads on their way
 // at once; the eight lanes of a head cover whole lines.  8192 tokens, 40 heads, d 128: 29.8 us (5.6 TB/s, 86 % of the measured copy);
 // with a table in shared memory for all heads of a token 42 (bank conflicts, a barrier), one head on its way at a time 45, eight 34,
-// four with the next four behind them 35 to 44.  12,300 tokens with their K and V into pages: 39.3 us (5.3 TB/s).
+// four with the next four behind them 35 to 44.  12,300 tokens with their K and V into pages: 39.3 us (5.3 TB/s);
+// 4500 in fp32 45.1 us (4.9 TB/s, cold).  Pair counts that are no multiple of a vector go element by element: the 8192 tokens above 49
+// to 51 us cold where vectors take 37, in fp32 62 to 66 where they take 60 to 66.
 // Small blocks: each goes through phases (loads, cosines, stores), and the more of them share an SM the better the phases mix; of 64, 128
 // and 256 threads at the same number of threads per SM 29.8 / 30.7 / 32.3 us, and 39.3 / 39.8 / 44.6 into pages.
 #include <type_traits>
