@@ -644,6 +644,8 @@ def dash_attn_evict_paged(p, mass, kv_len, page_table, Kpool, Vpool, kept, new_l
             and shape[1:] == lay.k[0][1:] and Kdst.stride() == lay.k[1] and Vdst.stride() == lay.v[1]):
         to = (shape[0], *lay.k[0][1:])         # the destination's pages: as many as there are, of the pools' size, heads and strides
         _misfits("dash_attn_evict_paged", Kpool=(Kpool, lay.k), Vpool=(Vpool, lay.v), Kdst=(Kdst, (to, lay.k[1])), Vdst=(Vdst, (to, lay.v[1])))
+    if not (0 <= sinks <= keep and 0 <= recent <= keep):         # (beyond 32 bits they would arrive as something else)
+        raise ValueError(f"dash_attn_evict_paged: sinks {sinks} and recent {recent} are parts of keep {keep}")
     rc = (_lib or lib()).dash_attn_evict_paged(
         ctypes.byref(p), keep, sinks, recent, mass.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), Kpool.data_ptr(), Vpool.data_ptr(),
         kept.data_ptr(), new_len.data_ptr(), dst_table.data_ptr(), width, shape[0], Kdst.data_ptr(), Vdst.data_ptr(),

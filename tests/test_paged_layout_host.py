@@ -170,3 +170,11 @@ def test_parameters_may_be_copied():
     q.h_q = 2
     with pytest.raises(ValueError):
         B.dash_attn_attend_chunk_paged(q, **calls["attend_chunk"])
+
+
+@pytest.mark.parametrize("kw", [dict(sinks=1 << 32), dict(recent=1 << 32), dict(sinks=-(1 << 32)), dict(sinks=(1 << 32) + 1, recent=-(1 << 32))])
+def test_counts_beyond_32_bits_are_not_cut_down(kw):
+    """ctypes keeps the low 32 bits of what it is given: 2^32 sinks would have been none."""
+    p, calls = _paged()
+    with pytest.raises(ValueError):
+        B.dash_attn_evict_paged(p, **{**calls["evict"], **kw})
